@@ -251,6 +251,137 @@ int terra_fixed_assignment_padding(int64_t H, int64_t W, int32_t p, int32_t alph
                                    int64_t* H_hat, int64_t* W_hat);
 int terra_ragged_window_range(int64_t M, int32_t ranks, int32_t r, int64_t* L, int64_t* R);
 
+/*
+ * ---- What stands around the attention in a Transformer block (Section IV-A: norm, projections, MLP) -----------------------------
+ * The paper names the block's parts and gives no formula; those below are this library's.  A pre-norm block is
+ *   norm -> QKV product (its output is the packed tensor) -> rotary positions in place -> terra_swin_attn_fwd_packed -> product onto the
+ *   residual -> norm -> product with activation -> product onto the residual,
+ * and its backward the same calls' backwards in reverse.  Activations, weights of products and their gradients "elem" are bf16, or fp16 with
+ * TERRA_DTYPE_F16; norm weights, biases, scales, and the gradients of all parameters are fp32.  Sums and everything between a call's
+ * inputs and outputs are fp32; each output is rounded once.  Tensors are dense, 16-byte aligned, without overlap unless said otherwise.
+ * The calls are reproducible run to run.
+ */
+
+/* Rows of `channels` (tokens x channels): 1 <= channels <= 16384, rows >= 1, eps >= 0 and finite. */
+typedef struct {
+    int64_t rows;
+    int32_t channels;
+    float eps;
+    int32_t dtype;                  /* of x, residual, h, y and their gradients: TERRA_DTYPE_*     */
+} terra_norm_desc;
+
+/*
+ * Root-mean-square norm with the residual's addition: h = x + residual, rstd = (mean over the channels of h^2 + eps)^(-1/2),
+ * y = h rstd weight.
+ *   x, residual   elem [rows, channels]; residual may be NULL: h = x
+ *   weight        fp32 [channels]
+ *   h             elem [rows, channels]   the sum, rounded (y and rstd are taken of the unrounded sum); may be NULL; may be x or residual
+ *   y             elem [rows, channels]   may be x or residual, not h
+ *   rstd          fp32 [rows]             what the backward call needs; may be NULL
+ * A row without a finite sum of squares gives what the formula gives: NaN, or zeros beside an infinite h.
+ */
+int terra_rms_norm_fwd(const terra_norm_desc* desc, const void* x, const void* residual, const float* weight, void* h, void* y, float* rstd,
+                       void* stream);
+/*
+ * The same with y in 8 bits, the operand of terra_linear_fwd_e4m3: scale = max over the row of |y| / 448, y8 = y / scale rounded to
+ * e4m3 (a row of zeros: scale 0, zeros).  A NaN in a row makes its scale and y8 NaN.
+ *   y8      e4m3 [rows, channels]
+ *   scale   fp32 [rows]
+ */
+int terra_rms_norm_fwd_e4m3(const terra_norm_desc* desc, const void* x, const void* residual, const float* weight, void* h, void* y8, float* scale,
+                            float* rstd, void* stream);
+/* Scratch bytes of terra_rms_norm_bwd.  Host-only. */
+int terra_rms_norm_workspace_bytes(const terra_norm_desc* desc, size_t* bytes);
+/*
+ * Backward: n = h rstd, g = d_y weight; d_x = rstd (g - n mean(g n)) + d_h, d_weight = sum over the rows of d_y n.  d_x is the gradient of x
+ * and of the residual alike.  (eps is not read.)
+ *   h, rstd   as the forward call left them (h = x where there was no residual)
+ *   d_y       elem [rows, channels]
+ *   d_h       elem [rows, channels]   gradient that reaches h past the norm; may be NULL
+ *   d_x       elem [rows, channels]   overwritten; may be d_y or d_h
+ *   d_weight  fp32 [channels]         overwritten
+ */
+int terra_rms_norm_bwd(const terra_norm_desc* desc, const void* h, const float* weight, const float* rstd, const void* d_y, const void* d_h, void* d_x,
+                       float* d_weight, void* workspace, size_t workspace_bytes, void* stream);
+
+#define TERRA_ACT_NONE 0
+#define TERRA_ACT_RELU 1
+#define TERRA_ACT_SILU 2        /* z / (1 + exp(-z)) */
+#define TERRA_ACT_GELU 3        /* z (1 + erf(z / sqrt 2)) / 2 */
+#define TERRA_ACT_GELU_TANH 4   /* z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2 */
+
+/* A product from n_in to n_out features: 1 <= n_in, n_out <= 65536, 1 <= rows <= 2^31 - 1024. */
+typedef struct {
+    int64_t rows;
+    int32_t n_in, n_out;
+    int32_t activation;             /* TERRA_ACT_*; forward: of this product; backward: the one that made x   */
+    int32_t dtype;                  /* TERRA_DTYPE_*                                                           */
+} terra_linear_desc;
+
+#define TERRA_LINEAR_FWD 0
+#define TERRA_LINEAR_FWD_E4M3 1
+#define TERRA_LINEAR_BWD 2
+/* Scratch bytes of a call (TERRA_LINEAR_*); 0 for most forward calls.  Host-only.  Rows that are no multiple of 16 bytes are copied to
+ * padded ones there, and the parts of a sum that is split over the GPU lie there. */
+int terra_linear_workspace_bytes(const terra_linear_desc* desc, int call, size_t* bytes);
+/*
+ * z = x w' + bias, y = act(z) + residual.
+ *   x          elem [rows, n_in]
+ *   w          elem [n_out, n_in]
+ *   bias       fp32 [n_out]; may be NULL
+ *   residual   elem [rows, n_out]; may be NULL
+ *   y          elem [rows, n_out]; may be residual
+ *   z          elem [rows, n_out]   for the backward through the activation; may be NULL
+ */
+int terra_linear_fwd(const terra_linear_desc* desc, const void* x, const void* w, const float* bias, const void* residual, void* y, void* z,
+                     void* workspace, size_t workspace_bytes, void* stream);
+/*
+ * The same with operands in 8 bits: z[i, j] = x_scale[i] w_scale[j] sum of x8 w8 + bias[j].
+ *   x8, w8    e4m3 [rows, n_in], [n_out, n_in]
+ *   x_scale   fp32 [rows], w_scale fp32 [n_out]
+ */
+int terra_linear_fwd_e4m3(const terra_linear_desc* desc, const void* x8, const float* x_scale, const void* w8, const float* w_scale, const float* bias,
+                          const void* residual, void* y, void* workspace, size_t workspace_bytes, void* stream);
+/*
+ * Backward.  d_z is the gradient of z: the upstream gradient itself where the product has no activation, and what the next product's
+ * backward gives as its d_x where the activation's z was handed to it, or terra_activation_bwd.
+ *   d_z      elem [rows, n_out]
+ *   z_in     elem [rows, n_in]   the z whose activation (desc->activation) x is: d_x is multiplied by act'(z_in); NULL: d_x is x's gradient
+ *   d_x      elem [rows, n_in]   d_z w act'(z_in); may be z_in; may be NULL
+ *   d_w      fp32 [n_out, n_in]  d_z' x; may be NULL
+ *   d_bias   fp32 [n_out]        sum over the rows of d_z; may be NULL
+ * w may be NULL where d_x is, x where d_w is.
+ */
+int terra_linear_bwd(const terra_linear_desc* desc, const void* x, const void* w, const void* d_z, const void* z_in, void* d_x, float* d_w, float* d_bias,
+                     void* workspace, size_t workspace_bytes, void* stream);
+/* d_z = d_y act'(z), elementwise over n elements; d_z may be d_y or z. */
+int terra_activation_bwd(int64_t n, int32_t activation, int32_t dtype, const void* z, const void* d_y, void* d_z, void* stream);
+
+#define TERRA_ROTARY_HALF 0          /* pair p: channels p and p + rot_dim / 2 of a head */
+#define TERRA_ROTARY_INTERLEAVED 1   /* pair p: channels 2 p and 2 p + 1 */
+/* How queries and keys are turned by their positions. */
+typedef struct {
+    int32_t rot_dim;                /* channels of a head that are turned, from the first on: even, 2 .. head_dim  */
+    int32_t layout;                 /* TERRA_ROTARY_*                                                              */
+    int32_t row_pairs;              /* 0 .. rot_dim / 2: the first pairs go by the token's row, the others by its column */
+    int32_t inverse;                /* 1: turn back (the backward call, on d_q and d_k)                            */
+    float scale;                    /* factor on the turned channels; finite                                       */
+} terra_rotary_desc;
+/*
+ * Pair p of every head becomes scale (a cos t - b sin t, a sin t + b cos t) with t = position inv_freq[p]; channels from rot_dim on are copied.
+ * The position is the token's row or column in the shifted frame, (u - shift_h) mod H and (v - shift_w) mod W, in which the tokens
+ * of a window are neighbours also across the seam, or the given one.
+ *   q, k        elem [B, H, W, heads, head_dim]; k (and k_out) may be NULL
+ *   inv_freq    fp64 [rot_dim / 2]      radians a step
+ *   positions   int32 [B, H, W, 2]      row and column of each token; may be NULL
+ *   q_out, k_out   as q, k; may be q, k
+ * The angle is formed in fp64, so positions far from the origin keep theirs.
+ */
+int terra_rotary(const terra_swin_desc* desc, const terra_rotary_desc* rotary, const double* inv_freq, const int32_t* positions, const void* q, const void* k,
+                 void* q_out, void* k_out, void* stream);
+/* The same in place on the packed layout [B, H, W, 3, heads, head_dim] of terra_swin_attn_fwd_packed (or its gradient); v is not touched. */
+int terra_rotary_packed(const terra_swin_desc* desc, const terra_rotary_desc* rotary, const double* inv_freq, const int32_t* positions, void* qkv, void* stream);
+
 /* Static text for a terra_status.  Host-only. */
 const char* terra_strerror(int status);
 

@@ -8,6 +8,7 @@ PyTorch is used for device memory and streams.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 
 import torch
@@ -19,7 +20,9 @@ EXPORTS = ("terra_route_sizes", "terra_window_route", "terra_swin_workspace_byte
            "terra_swin_attn_fwd_noalloc", "terra_swin_attn_bwd", "terra_swin_check", "terra_strerror", "terra_last_cuda_error",
            "terra_launch_count", "terra_selftest_bounded_wait", "terra_profile_enable", "terra_profile_count", "terra_profile_get",
            "terra_fixed_assignment_padding", "terra_ragged_window_range", "terra_swin_attn_fwd_packed", "terra_swin_attn_bwd_packed",
-           "terra_pad_grid", "terra_crop_grid")
+           "terra_pad_grid", "terra_crop_grid", "terra_rms_norm_fwd", "terra_rms_norm_fwd_e4m3", "terra_rms_norm_workspace_bytes", "terra_rms_norm_bwd",
+           "terra_linear_workspace_bytes", "terra_linear_fwd", "terra_linear_fwd_e4m3", "terra_linear_bwd", "terra_activation_bwd",
+           "terra_rotary", "terra_rotary_packed")
 
 
 class TerraError(RuntimeError):
@@ -34,6 +37,20 @@ class terra_swin_desc(ctypes.Structure):
                [("scale", ctypes.c_float), ("dtype", ctypes.c_int32)]
 
 TERRA_DTYPE_BF16, TERRA_DTYPE_F16 = 0, 1
+ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}
+ROTARY_LAYOUTS = {"half": 0, "interleaved": 1}
+
+
+class terra_norm_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("channels", ctypes.c_int32), ("eps", ctypes.c_float), ("dtype", ctypes.c_int32)]
+
+
+class terra_linear_desc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in ("n_in", "n_out", "activation", "dtype")]
+
+
+class terra_rotary_desc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("rot_dim", "layout", "row_pairs", "inverse")] + [("scale", ctypes.c_float)]
 
 
 _lib = None
@@ -80,6 +97,16 @@ def load_library(path: str | None = None) -> ctypes.CDLL:
     for n in ("terra_pad_grid", "terra_crop_grid"):
         getattr(lib, n).argtypes = [vp, vp] + [ctypes.c_int32] * 5 + [ctypes.c_int64, vp]
         getattr(lib, n).restype = ctypes.c_int
+    np_, lp, rp, sp, i64 = (ctypes.POINTER(terra_norm_desc), ctypes.POINTER(terra_linear_desc), ctypes.POINTER(terra_rotary_desc),
+                            ctypes.POINTER(ctypes.c_size_t), ctypes.c_int64)
+    for n, args in (("terra_rms_norm_fwd", [np_] + [vp] * 7), ("terra_rms_norm_fwd_e4m3", [np_] + [vp] * 8), ("terra_rms_norm_workspace_bytes", [np_, sp]),
+                    ("terra_rms_norm_bwd", [np_] + [vp] * 8 + [ctypes.c_size_t, vp]), ("terra_linear_workspace_bytes", [lp, ctypes.c_int, sp]),
+                    ("terra_linear_fwd", [lp] + [vp] * 7 + [ctypes.c_size_t, vp]), ("terra_linear_fwd_e4m3", [lp] + [vp] * 8 + [ctypes.c_size_t, vp]),
+                    ("terra_linear_bwd", [lp] + [vp] * 8 + [ctypes.c_size_t, vp]),
+                    ("terra_activation_bwd", [i64, ctypes.c_int32, ctypes.c_int32] + [vp] * 4),
+                    ("terra_rotary", [dp, rp] + [vp] * 7), ("terra_rotary_packed", [dp, rp] + [vp] * 4)):
+        getattr(lib, n).argtypes = args
+        getattr(lib, n).restype = ctypes.c_int
     if path is None:
         _bind_host(lib)
         _lib = lib
@@ -97,7 +124,9 @@ def _bind_host(lib) -> None:
     from . import _host as module
     module.bind(*[ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in
                   ("terra_swin_workspace_bytes", "terra_swin_attn_fwd", "terra_swin_attn_bwd", "terra_swin_attn_fwd_packed",
-                   "terra_swin_attn_bwd_packed", "terra_swin_attn_fwd_noalloc")], _check)
+                   "terra_swin_attn_bwd_packed", "terra_swin_attn_fwd_noalloc", "terra_rms_norm_fwd", "terra_rms_norm_fwd_e4m3",
+                   "terra_rms_norm_workspace_bytes", "terra_rms_norm_bwd", "terra_linear_workspace_bytes", "terra_linear_fwd", "terra_linear_fwd_e4m3",
+                   "terra_linear_bwd", "terra_activation_bwd", "terra_rotary", "terra_rotary_packed")], _check)
     _host = module
 
 
@@ -260,3 +289,106 @@ def terra_crop_grid(y, H: int, W: int):
     x = torch.empty((B, H, W) + tuple(y.shape[3:]), dtype=y.dtype, device=y.device)
     _check(load_library().terra_crop_grid(_ptr(y), _ptr(x), B, H, W, H_pad, W_pad, token_bytes, _stream()))
     return x
+
+
+def _code(names: dict, name: str, what: str) -> int:
+    code = names.get(name)
+    if code is None:
+        raise ValueError(f"terra: {what} must be one of {', '.join(names)}, got {name!r}")
+    return code
+
+
+def terra_rms_norm_fwd(x, weight, residual=None, eps=1e-6, h=None, y=None, rstd=None):
+    """h = x + residual, y = h weight / sqrt(mean(h^2) + eps) over the last dimension.  x, residual bf16 or fp16 [..., channels]; weight fp32
+    [channels].  Returns (y like x, h like x, rstd fp32 [rows]); without a residual h is x itself."""
+    return (_host or _native()).norm_fwd(x, weight, residual, eps, h, y, rstd)
+
+
+def terra_rms_norm_fwd_e4m3(x, weight, residual=None, eps=1e-6, h=None, y=None, scale=None):
+    """The same with y in 8 bits.  Returns (y float8_e4m3fn like x, scale fp32 [rows], h like x): y stands for y * scale."""
+    return (_host or _native()).norm_fwd_e4m3(x, weight, residual, eps, h, y, scale)
+
+
+def terra_rms_norm_bwd(h, weight, rstd, d_y, d_h=None, d_x=None, d_weight=None, workspace=None):
+    """Backward of terra_rms_norm_fwd.  d_h: the gradient that reaches h past the norm.  Returns (d_x like h, the gradient of x and of the
+    residual alike, d_weight fp32 [channels])."""
+    return (_host or _native()).norm_bwd(h, weight, rstd, d_y, d_h, d_x, d_weight, workspace)
+
+
+def terra_rms_norm_workspace_bytes(rows: int, channels: int, dtype=torch.bfloat16) -> int:
+    n = ctypes.c_size_t()
+    desc = terra_norm_desc(rows, channels, 0.0, TERRA_DTYPE_F16 if dtype == torch.float16 else TERRA_DTYPE_BF16)
+    _check(load_library().terra_rms_norm_workspace_bytes(ctypes.byref(desc), ctypes.byref(n)))
+    return int(n.value)
+
+
+def terra_linear_fwd(x, w, bias=None, residual=None, activation="none", keep_z=False, y=None, z=None, workspace=None):
+    """z = x w' + bias, y = act(z) + residual.  x bf16 or fp16 [..., n_in], w [n_out, n_in], residual [..., n_out] of its type; bias fp32
+    [n_out].  Returns (y [..., n_out], z like y if keep_z, else None)."""
+    return (_host or _native()).linear_fwd(x, w, bias, residual, _code(ACTIVATIONS, activation, "activation"), keep_z, y, z, workspace)
+
+
+def terra_linear_fwd_e4m3(x, x_scale, w, w_scale, bias=None, residual=None, activation="none", dtype=torch.bfloat16, y=None, workspace=None):
+    """The same on float8_e4m3fn operands, x [..., n_in] with x_scale fp32 [rows], w [n_out, n_in] with w_scale fp32 [n_out]: an operand stands for
+    its value times its row's scale (terra_rms_norm_fwd_e4m3 gives x so).  Returns y of `dtype`."""
+    if dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError("terra: activations are bf16 or fp16")
+    return (_host or _native()).linear_fwd_e4m3(x, x_scale, w, w_scale, bias, residual, _code(ACTIVATIONS, activation, "activation"),
+                                                TERRA_DTYPE_F16 if dtype == torch.float16 else TERRA_DTYPE_BF16, y, workspace)
+
+
+def terra_linear_bwd(x, w, d_z, z_in=None, activation="none", need_dx=True, need_dw=True, need_dbias=True, d_x=None, d_w=None, d_bias=None, workspace=None):
+    """Backward of terra_linear_fwd from d_z, the gradient of its z.  With z_in, x is act(z_in) and d_x the gradient of z_in.  Returns
+    (d_x like x, d_w fp32 [n_out, n_in], d_bias fp32 [n_out]), None for what is not needed."""
+    return (_host or _native()).linear_bwd(x, w, d_z, z_in, _code(ACTIVATIONS, activation, "activation"), need_dx, need_dw, need_dbias, d_x, d_w, d_bias, workspace)
+
+
+def terra_linear_workspace_bytes(rows: int, n_in: int, n_out: int, call: str = "fwd") -> int:
+    """Scratch bytes of a "fwd", "fwd_e4m3" or "bwd" call."""
+    n = ctypes.c_size_t()
+    code = _code({"fwd": 0, "fwd_e4m3": 1, "bwd": 2}, call, "call")
+    _check(load_library().terra_linear_workspace_bytes(ctypes.byref(terra_linear_desc(rows, n_in, n_out, 0, 0)), code, ctypes.byref(n)))
+    return int(n.value)
+
+
+def terra_activation_bwd(z, d_y, activation, d_z=None):
+    """d_z = d_y act'(z): for an activation that no product follows (terra_linear_bwd does it in the product's epilogue)."""
+    return (_host or _native()).activation_bwd(z, d_y, _code(ACTIVATIONS, activation, "activation"), d_z)
+
+
+def terra_rotary(desc, q, k, inv_freq, row_pairs=0, layout="half", scale=1.0, positions=None, inverse=False, q_out=None, k_out=None):
+    """Turns the first 2 len(inv_freq) channels of each head of q and k (None: q alone) by position x inv_freq (fp64): the first row_pairs
+    pairs by the token's row, the others by its column, in the shifted frame or as `positions` (int32 [B, H, W, 2]) has them.
+    Returns (q_out, k_out); pass q and k themselves to turn them in place.  inverse=True is the backward."""
+    return (_host or _native()).rotary(desc, q, k, inv_freq, row_pairs, _code(ROTARY_LAYOUTS, layout, "layout"), scale, inverse, positions, q_out, k_out)
+
+
+def terra_rotary_packed(desc, qkv, inv_freq, row_pairs=0, layout="half", scale=1.0, positions=None, inverse=False):
+    """The same in place on q and k of the packed tensor [B, H, W, 3, heads, head_dim] (or of its gradient).  Returns qkv."""
+    return (_host or _native()).rotary_packed(desc, qkv, inv_freq, row_pairs, _code(ROTARY_LAYOUTS, layout, "layout"), scale, inverse, positions)
+
+
+def rotary_frequencies(rot_dim: int, row_pairs: int = 0, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, length: float = 0.0,
+                       fast: float = 32.0, slow: float = 1.0, device="cuda"):
+    """(inv_freq fp64 [rot_dim / 2], scale) for terra_rotary.  Each axis (row_pairs pairs by row, the others by column) has n pairs of its own with
+    base^(-i / n), i = 0 .. n - 1.  For positions `factor` times as far as a model was trained on:
+      "linear"  every frequency divided by factor;
+      "base"    base times factor^(n / (n - 1)): the fastest pair stays, the slowest is divided by factor;
+      "parts"   pairs that turn more than `fast` times over the trained `length` stay, those that turn less than `slow` times are divided
+                by factor, linearly between; scale = 1 + 0.1 ln(factor)."""
+    if scaling not in ("none", "linear", "base", "parts"):
+        raise ValueError(f"terra: scaling must be one of none, linear, base, parts, got {scaling!r}")
+    if rot_dim < 2 or rot_dim % 2 or not 0 <= row_pairs <= rot_dim // 2 or base <= 0 or factor < 1 or (scaling == "parts" and (length <= 0 or fast <= slow)):
+        raise ValueError("terra: rot_dim must be even and hold row_pairs, base positive, factor at least 1, length positive and fast above slow")
+    freq = []
+    for n in (row_pairs, rot_dim // 2 - row_pairs):
+        b = base * factor ** (n / (n - 1)) if scaling == "base" and n > 1 else base
+        for i in range(n):
+            f = b ** (-i / n)
+            if scaling == "linear":
+                f /= factor
+            elif scaling == "parts":
+                kept = min(1.0, max(0.0, (length * f / (2 * math.pi) - slow) / (fast - slow)))
+                f = f * kept + f / factor * (1 - kept)
+            freq.append(f)
+    return torch.tensor(freq, dtype=torch.float64, device=device), 1.0 + 0.1 * math.log(factor) if scaling == "parts" else 1.0

@@ -8,6 +8,7 @@
 #include <cstring>
 
 #include "../../include/terra.h"
+#include "block_kernels.h"
 #include "swin_kernels.h"
 
 namespace terra {
@@ -359,7 +360,7 @@ int terra_swin_check(void* stream) {
     e = read_bwd_tc_status(&timed_out_bwd);
     if (e != cudaSuccess) return cuda_fail(e, "terra_swin_check");
     // the fp16 builds of the same kernels keep status words of their own
-    int t16[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    int t16[10] = {0, 0, 0, 0, 0, 0, 0, 0, 0, 0};
     e = read_tc_status_f16(&t16[0], (cudaStream_t)stream);
     if (e == cudaSuccess) e = read_bwd_tc_status_f16(&t16[1]);
     if (e == cudaSuccess) e = read_bwd_onepass_status_f16(&t16[2]);
@@ -368,6 +369,8 @@ int terra_swin_check(void* stream) {
     if (e == cudaSuccess) e = read_fwd_win_status(&t16[5]);
     if (e == cudaSuccess) e = read_fwd_tc64_status_f16(&t16[6]);
     if (e == cudaSuccess) e = read_fwd_tc64_status(&t16[7]);
+    if (e == cudaSuccess) e = read_linear_status_f16(&t16[8]);
+    if (e == cudaSuccess) e = read_linear_status(&t16[9]);
     if (e != cudaSuccess) return cuda_fail(e, "terra_swin_check");
     bool any16 = false;
     for (int t : t16) any16 = any16 || t;
