@@ -64,6 +64,84 @@ __device__ __forceinline__ float act_slope(float z) {
     return 1.f;
 }
 
+// ---- two at a time (one instruction for a pair of additions or products, sm_100) --------------------------------
+typedef unsigned long long Pair;                       // two fp32
+__device__ __forceinline__ Pair pair_of(float a, float b) { Pair p; asm("mov.b64 %0, {%1, %2};\n" : "=l"(p) : "f"(a), "f"(b)); return p; }
+__device__ __forceinline__ Pair both(float a) { return pair_of(a, a); }
+__device__ __forceinline__ void split_pair(Pair p, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;\n" : "=f"(a), "=f"(b) : "l"(p)); }
+__device__ __forceinline__ Pair pfma(Pair a, Pair b, Pair c) { Pair d; asm("fma.rn.f32x2 %0, %1, %2, %3;\n" : "=l"(d) : "l"(a), "l"(b), "l"(c)); return d; }
+__device__ __forceinline__ Pair padd(Pair a, Pair b) { Pair d; asm("add.rn.f32x2 %0, %1, %2;\n" : "=l"(d) : "l"(a), "l"(b)); return d; }
+__device__ __forceinline__ Pair pmul(Pair a, Pair b) { Pair d; asm("mul.rn.f32x2 %0, %1, %2;\n" : "=l"(d) : "l"(a), "l"(b)); return d; }
+__device__ __forceinline__ Pair prcp(Pair p) { float a, b; split_pair(p, a, b); return pair_of(fast_rcp(a), fast_rcp(b)); }
+__device__ __forceinline__ Pair pexp2(Pair p) { float a, b; split_pair(p, a, b); return pair_of(fast_exp2(a), fast_exp2(b)); }
+// |x| up to `most`, a NaN stays one
+__device__ __forceinline__ float abs_upto(float x, float most) { float y; asm("min.NaN.f32 %0, %1, %2;\n" : "=f"(y) : "f"(fabsf(x)), "f"(most)); return y; }
+__device__ __forceinline__ float clamp_nan(float x, float most) {
+    float y;
+    asm("{\n\t.reg .f32 t;\n\tmin.NaN.f32 t, %1, %2;\n\tmax.NaN.f32 %0, t, %3;\n\t}\n" : "=f"(y) : "f"(x), "f"(most), "f"(-most));
+    return y;
+}
+
+// normal_tail of |x| = a (a <= 100)
+__device__ __forceinline__ void normal_tail2(Pair a, Pair& bell, Pair& tail) {
+    const Pair t = prcp(pfma(a, both(0.65f * 0.70710678f), both(1.f)));
+    bell = pexp2(pmul(pmul(a, both(-0.5f * kLog2e)), a));
+    Pair g = pfma(both(0.5f * 0.14364023f), t, both(0.5f * -0.47167895f));
+    g = pfma(g, t, both(0.5f * 0.35566068f));
+    g = pfma(g, t, both(0.5f * 0.23218703f));
+    g = pfma(g, t, both(0.5f * 0.37380508f));
+    g = pfma(g, t, both(0.5f * 0.36639139f));
+    tail = pmul(pmul(g, t), bell);
+}
+__device__ __forceinline__ Pair sigmoid2(Pair log2e_x) {           // of x, given x log2(e)
+    float a, b;
+    split_pair(log2e_x, a, b);
+    return prcp(padd(both(1.f), pair_of(fast_exp2(-a), fast_exp2(-b))));
+}
+
+template <int ACT>
+__device__ __forceinline__ Pair act2(Pair z) {
+    float a, b;
+    split_pair(z, a, b);
+    if (ACT == TERRA_ACT_RELU) return pair_of(a < 0.f ? 0.f : a, b < 0.f ? 0.f : b);
+    if (ACT == TERRA_ACT_SILU) return pmul(z, sigmoid2(pmul(z, both(kLog2e))));
+    if (ACT == TERRA_ACT_GELU) {       // max(z, 0) - |z| tail; beyond 100 the tail is 0 in fp32, and |z| may be infinite
+        const Pair m = pair_of(abs_upto(a, 100.f), abs_upto(b, 100.f));
+        Pair bell, tail;
+        normal_tail2(m, bell, tail);
+        return pfma(pmul(m, both(-1.f)), tail, pair_of(fmaxf(a, 0.f), fmaxf(b, 0.f)));
+    }
+    if (ACT == TERRA_ACT_GELU_TANH)
+        return pmul(z, sigmoid2(pmul(z, pfma(pmul(z, z), both(2.f * kGeluTanhA * kLog2e * kGeluTanhB), both(2.f * kGeluTanhA * kLog2e)))));
+    return z;
+}
+
+template <int ACT>
+__device__ __forceinline__ Pair act_slope2(Pair z) {
+    float a, b;
+    split_pair(z, a, b);
+    if (ACT == TERRA_ACT_RELU) return pair_of(a > 0.f ? 1.f : 0.f, b > 0.f ? 1.f : 0.f);
+    if (ACT == TERRA_ACT_GELU) {
+        const Pair m = pair_of(abs_upto(a, 100.f), abs_upto(b, 100.f));
+        Pair bell, tail;
+        normal_tail2(m, bell, tail);
+        // Phi(z) + z phi(z): tail - |z| phi below 0, 1 less that above
+        const Pair low = pfma(pmul(m, both(-0.3989422804f)), bell, tail);
+        float u, v;
+        split_pair(low, u, v);
+        return pair_of(a < 0.f ? u : 1.f - u, b < 0.f ? v : 1.f - v);
+    }
+    if (ACT == TERRA_ACT_SILU || ACT == TERRA_ACT_GELU_TANH) {     // beyond 100 (30 for the cube) s (1 - s) is 0 in fp32
+        const Pair c = pair_of(clamp_nan(a, 100.f), clamp_nan(b, 100.f)), cc = pmul(c, c);
+        const float k = 2.f * kGeluTanhA;
+        const Pair s = ACT == TERRA_ACT_SILU ? sigmoid2(pmul(c, both(kLog2e)))
+                                             : sigmoid2(pmul(c, pfma(cc, both(k * kLog2e * kGeluTanhB), both(k * kLog2e))));
+        const Pair rest = pmul(pmul(c, s), pfma(s, both(-1.f), both(1.f)));
+        return ACT == TERRA_ACT_SILU ? padd(s, rest) : pfma(rest, pfma(cc, both(3.f * k * kGeluTanhB), both(k)), s);
+    }
+    return both(1.f);
+}
+
 // f(integral constant of the activation)
 template <int N> struct ActTag { static constexpr int value = N; };
 template <class F>

@@ -8,6 +8,24 @@
 
 namespace terra {
 
+// n / d for 0 <= n < 2^31, d >= 1, by a multiplication: with 2^(l - 1) < d <= 2^l, m = floor(2^(31 + l) / d) + 1 is less than 2^32 and
+// exceeds 2^(31 + l) / d by at most 1, so n m / 2^(31 + l) exceeds n / d by less than 2^-l <= 1 / d.
+struct Divider {
+    uint32_t d, m, shift;
+    __host__ explicit Divider(uint32_t by) : d(by), m(0), shift(0) {
+        uint32_t l = 0;
+        while ((1ull << l) < by) ++l;
+        if (by > 1) {
+            m = (uint32_t)((1ull << (31 + l)) / by + 1);
+            shift = l - 1;
+        }
+    }
+    __device__ __forceinline__ void split(uint32_t n, uint32_t& quo, uint32_t& rem) const {
+        quo = d > 1 ? __umulhi(n, m) >> shift : n;
+        rem = n - quo * d;
+    }
+};
+
 // ---- root-mean-square norm (norm.cu) ----------------------------------------------------------------------------
 constexpr int kNormMaxChannels = 16384;
 struct NormArgs {

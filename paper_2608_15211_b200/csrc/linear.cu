@@ -8,12 +8,13 @@
 // Persistent: a unit is one output tile (of one part of the sum, where it is split).  PAIR: two CTAs on neighbouring SMs work on a
 // tile of 256 rows with tcgen05.mma.cta_group::2, each with its 128 rows of A and half of the columns of B; alone, a CTA has 128 rows.  Five
 // stages of 64 k (128 in e4m3) each, two accumulators in TMEM, so that the epilogue of a tile runs under the products of the next.
-// The epilogue turns a warp's 32 rows x 64 columns over in shared memory, so that all it reads and writes in global memory is runs of whole rows.
+// The epilogue works on a warp's 32 rows x 64 columns at a time, a row to a thread, two columns to an instruction; the residual comes and the
+// results go as tiles in shared memory that the copy engine moves (rows that are no multiples of 16 bytes: the warp itself, in whole rows).
 //
 // The tensor cores' sum over k is not rounded to nearest, and its error grows with the number of steps.  The weight gradient, a sum over all
 // rows that comes out in fp32, therefore leaves TMEM every kChunk stages and is added up in registers.
 //
-// Roles (384 threads): warp 0 copies, warp 1 issues the products, warp 2 has the TMEM, warps 4-11 the epilogue.
+// Roles (640 threads): warp 0 copies, warp 1 issues the products, warp 2 has the TMEM, warps 4-19 the epilogue.
 // Every mbarrier wait is bounded; on expiry the CTA raises an abort flag, all roles leave their loops, TMEM is released and the host reads
 // the device status word.
 #include <cuda.h>
@@ -37,14 +38,20 @@ namespace {
 
 using namespace tc;
 
-constexpr int kThreads = 384;
-constexpr int kEpiWarp0 = 4, kEpiWarps = 8;
+constexpr int kEpiWarp0 = 4, kEpiWarpsMost = 16;
+// Groups of four epilogue warps, one for each 32 lanes of TMEM, and the registers of a thread at launch, in the epilogue and elsewhere
+template <int KIND> struct Roles {
+    static constexpr int kGroups = 4, kEpiWarps = 4 * kGroups, kThreads = 32 * (kEpiWarp0 + kEpiWarps);
+    static constexpr int kRegsLaunch = 96, kRegsEpi = 104, kRegsOther = 64;
+    static_assert(kEpiWarps * kRegsEpi + kEpiWarp0 * kRegsOther <= (kEpiWarps + kEpiWarp0) * kRegsLaunch, "register hand-over does not balance");
+};
 constexpr int kStages = 5;
 constexpr int kOperand = 128 * 128;                    // bytes of an operand's stage: 128 rows (or columns) x 128 bytes
-constexpr int kTurn = 32 * 64 * 4;                     // a warp's 32 x 64 fp32
-constexpr int kOffTurn = kStages * 2 * kOperand;
-constexpr int kOffBars = kOffTurn + kEpiWarps * kTurn;
-constexpr int kBFull = 0, kBEmpty = kStages, kBAccFull = 2 * kStages, kBAccEmpty = kBAccFull + 2, kBCount = kBAccEmpty + 2;
+constexpr int kTile = 32 * 128;                        // a warp's 32 rows x 64 columns of 16-bit elements, or 32 columns of 32-bit ones
+constexpr int kOffTiles = kStages * 2 * kOperand;
+constexpr int kOffBars = kOffTiles + kEpiWarpsMost * kTile;
+constexpr int kBFull = 0, kBEmpty = kStages, kBAccFull = 2 * kStages, kBAccEmpty = kBAccFull + 2, kBIn = kBAccEmpty + 2,
+              kBCount = kBIn + kEpiWarpsMost;
 constexpr int kOffTmem = kOffBars + 8 * kBCount, kOffAbort = kOffTmem + 4;
 constexpr int kSmem = kOffAbort + 4 + 1024;            // the base is rounded up to 1 KB
 constexpr int kAccCols = 256;                          // TMEM columns between the two accumulators
@@ -71,20 +78,18 @@ __device__ __forceinline__ void load_box(uint32_t dst, const void* map, int x, i
     else
         tma_load_2d(dst, map, x, y, bar);
 }
+// D[tmem] (+)= A B; descriptors as their low words (start address and leading dimension) and the high words that all of a kind share
+#define TERRA_MMA(GROUP, KIND)                                                                                                       \
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tmov.b64 da, {%1, %3};\n\tmov.b64 db, {%2, %3};\n\tsetp.ne.b32 p, %5, 0;\n\t" \
+                 "tcgen05.mma.cta_group::" GROUP ".kind::" KIND " [%0], da, db, %4, p;\n\t}\n" ::"r"(d), "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate) : "memory")
 template <bool PAIR, bool E4M3>
-__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-    if (PAIR && E4M3)
-        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}\n"
-                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
-    else if (PAIR)
-        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}\n"
-                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
-    else if (E4M3)
-        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}\n"
-                     ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
-    else
-        mma_ss(d, a, b, idesc, accumulate);
+__device__ __forceinline__ void mma(uint32_t d, uint32_t a_lo, uint32_t b_lo, uint32_t hi, uint32_t idesc, uint32_t accumulate) {
+    if (PAIR && E4M3) TERRA_MMA("2", "f8f6f4");
+    else if (PAIR) TERRA_MMA("2", "f16");
+    else if (E4M3) TERRA_MMA("1", "f8f6f4");
+    else TERRA_MMA("1", "f16");
 }
+#undef TERRA_MMA
 // arrives on `bar`, at its place in both CTAs of a pair, once all products issued so far are complete
 template <bool PAIR>
 __device__ __forceinline__ void commit(uint32_t bar) {
@@ -97,147 +102,192 @@ __device__ __forceinline__ void commit(uint32_t bar) {
 template <bool PAIR>
 __device__ __forceinline__ void arrive_leader(uint32_t bar) {
     if (PAIR)
-        asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];\n" ::"r"(leaders(bar)) : "memory");
+        // (relaxed: what the arrival is about, reads of TMEM, has been waited for; a release would wait for all of the warp's stores, 2000 cycles)
+        asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];\n" ::"r"(leaders(bar)) : "memory");
     else
         mbar_arrive(bar);
 }
 
-struct Maps { CUtensorMap a, b; };
+struct Maps { CUtensorMap a, b, in, y, z; };       // in: the residual or z_in
+__device__ __forceinline__ void store_box(const void* map, int x, int y, uint32_t src) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];\n" ::"l"(map), "r"(x), "r"(y), "r"(src) : "memory");
+}
+__device__ __forceinline__ void stores_commit() { asm volatile("cp.async.bulk.commit_group;\n" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void stores_read() { asm volatile("cp.async.bulk.wait_group.read %0;\n" ::"n"(N) : "memory"); }   // all but the last N
 
 struct Job {
     long long M;
     int N;
     int bn;                                    // columns of a tile: a multiple of 32
-    int m_tiles, n_tiles, group;               // tiles are walked through in groups of `group` rows of tiles
+    int m_tiles, n_tiles, group, groups;       // tiles are walked through in groups of `group` rows of tiles
     int splits, k_blocks, kb_per_split;
     int bytes_b;                               // of a CTA's share of B in a stage
     int boxes_b;                               // MN-major: boxes of 64 columns
     uint32_t idesc;
+    int by_map;                                // rows of the outputs are multiples of 16 bytes: the copy engine moves them
     LinearEpilogue e;
 };
 
-struct Unit { long long m0; int n0, k0, k1, split; };
-
-__device__ __forceinline__ Unit unit_at(const Job& j, long long u, int tile_rows) {
-    const int per_split = j.m_tiles * j.n_tiles;
-    long long split, rest;
-    int tile;
-    split_item(u, per_split, split, tile);
-    const int per_group = j.group * j.n_tiles, g = tile / per_group, first = g * j.group, rows = min(j.group, j.m_tiles - first);
-    rest = tile - g * per_group;
-    const int n = (int)rest / rows, m = first + (int)rest - n * rows;
-    Unit r;
-    r.m0 = (long long)m * tile_rows;
-    r.n0 = n * j.bn;
-    r.split = (int)split;
-    r.k0 = r.split * j.kb_per_split;
-    r.k1 = min(j.k_blocks, r.k0 + j.kb_per_split);
-    return r;
+// A unit as digits: the row of tiles within its group (fastest), the column of tiles, the group, the part of the sum.  Going `step` units on adds the
+// step's digits with carries.  (Divisions, in every role for every tile, cost each tile 700 cycles, 64-bit ones 1500.)  The last group
+// may have fewer rows than the others: its units beyond are there and empty.
+struct Digits { int m, n, g, split; };
+__device__ __forceinline__ Digits digits_of(const Job& j, uint32_t u) {
+    Digits d;
+    d.m = (int)(u % j.group);
+    u /= j.group;
+    d.n = (int)(u % j.n_tiles);
+    u /= j.n_tiles;
+    d.g = (int)(u % j.groups);
+    d.split = (int)(u / j.groups);
+    return d;
 }
+struct Units {
+    const Job& j;
+    Digits at, step;
+    __device__ __forceinline__ Units(const Job& job, uint32_t first, uint32_t by) : j(job), at(digits_of(job, first)), step(digits_of(job, by)) {}
+    __device__ __forceinline__ bool there() const { return at.split < j.splits; }
+    __device__ __forceinline__ bool empty() const { return at.g * j.group + at.m >= j.m_tiles; }
+    __device__ __forceinline__ void advance() {
+        at.m += step.m;
+        int carry = at.m >= j.group;
+        at.m -= carry ? j.group : 0;
+        at.n += step.n + carry;
+        carry = at.n >= j.n_tiles;
+        at.n -= carry ? j.n_tiles : 0;
+        at.g += step.g + carry;
+        carry = at.g >= j.groups;
+        at.g -= carry ? j.groups : 0;
+        at.split += step.split + carry;
+    }
+    __device__ __forceinline__ void next() {           // the next one that is not empty, or the end
+        do advance();
+        while (there() && empty());
+    }
+    __device__ __forceinline__ void settle() {         // from an empty first one on
+        if (there() && empty()) next();
+    }
+    __device__ __forceinline__ long long m0(int tile_rows) const { return (long long)(at.g * j.group + at.m) * tile_rows; }
+    __device__ __forceinline__ int n0() const { return at.n * j.bn; }
+    __device__ __forceinline__ int k0() const { return at.split * j.kb_per_split; }
+    __device__ __forceinline__ int k1() const { return min(j.k_blocks, (at.split + 1) * j.kb_per_split); }
+};
 
-__device__ __forceinline__ float4 elems4(uint2 v) {
-    const float2 a = elem2_to_float2(v.x), b = elem2_to_float2(v.y);
-    return make_float4(a.x, a.y, b.x, b.y);
+// Two neighbouring columns of D to z and y.  `in`: the residual's or the activation input's two elements.
+template <int KIND, int ACT, bool E4M3>
+__device__ __forceinline__ Pair finish2(Pair d, Pair bias, Pair scale, Pair in, Pair& z) {
+    if (KIND == kLinearInput) return pmul(d, act_slope2<ACT>(in));
+    z = E4M3 ? pfma(d, scale, bias) : padd(d, bias);
+    return padd(act2<ACT>(z), in);
 }
+__device__ __forceinline__ Pair elems2(uint32_t v) { const float2 t = elem2_to_float2(v); return pair_of(t.x, t.y); }
+__device__ __forceinline__ uint32_t pack2(Pair p) { float a, b; split_pair(p, a, b); return pack_elem(a, b); }
 
-// What is made of four neighbouring columns of D.  `r`, `z`: the residual's or the activation input's four elements.
-template <int KIND, int ACT>
-__device__ __forceinline__ void finish4(float (&v)[4], const float4& bias, const float4& ws, float xs, const float4& in, bool scaled, float (&z)[4]) {
-    const float b[4] = {bias.x, bias.y, bias.z, bias.w}, w[4] = {ws.x, ws.y, ws.z, ws.w}, t[4] = {in.x, in.y, in.z, in.w};
+__device__ float g_zeros[64];          // what stands for a bias that is not there
+
+// p[col .. col + 15], the same for all threads of a warp; from the n-th value on some that is there
+__device__ __forceinline__ void row_values(const float* p, int col, int n, float (&v)[16]) {
+    if (col + 16 <= n) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if (KIND == kLinearForward) {
-            z[i] = scaled ? fmaf(v[i] * xs, w[i], b[i]) : v[i] + b[i];
-            v[i] = act<ACT>(z[i]) + t[i];
-        } else {
-            v[i] *= act_slope<ACT>(t[i]);
+        for (int q = 0; q < 4; ++q) {
+            const float4 t = __ldg(reinterpret_cast<const float4*>(p + col) + q);
+            v[4 * q] = t.x; v[4 * q + 1] = t.y; v[4 * q + 2] = t.z; v[4 * q + 3] = t.w;
         }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = __ldg(p + min(col + i, n - 1));
     }
 }
 
-// One warp's rows x 64 columns, out of its turned-over tile (`v4(i)`: columns 4 j .. 4 j + 3 of row 2 i + lane / 16, j = lane % 16) to global memory.
-// `row0`: the row of i = 0, lane 0; `col0`: the column of j = 0; columns from `cols` on belong to others.
-template <int KIND, int ACT, class V>
-__device__ __forceinline__ void write_rows(const LinearEpilogue& e, long long M, int N, long long row0, int col0, int cols, int lane, V v4) {
-    const int j = lane & 15, col = col0 + 4 * j;
-    const long long row_a = row0 + (lane >> 4);
-    const bool in_col = 4 * j < cols && col < N;
-    const uint16_t* extra = (const uint16_t*)(KIND == kLinearForward ? e.residual : e.z_in);
-    float4 bias = make_float4(0.f, 0.f, 0.f, 0.f), ws = bias;
-    if ((N & 3) == 0) {
-        if (in_col && KIND == kLinearForward && e.bias) bias = *reinterpret_cast<const float4*>(e.bias + col);
-        if (in_col && KIND == kLinearForward && e.w_scale) ws = *reinterpret_cast<const float4*>(e.w_scale + col);
+// Where a warp's tile keeps 16 bytes: rows of 128 bytes (64 columns) or 64 (32 columns), whose 16-byte places are exchanged by the row's
+// number, as the copy engine does it.
+__device__ __forceinline__ uint32_t place(int row, int at, bool narrow) {
+    return narrow ? row * 64 + ((at ^ ((row >> 1) & 3)) << 4) : row * 128 + ((at ^ (row & 7)) << 4);
+}
+
+// A warp's tile <-> `rows` rows of global memory from g on (its first row and column; rows of `stride` elements), the first `cols` columns, in units
+// of T: for rows that are no multiples of 16 bytes, and tiles that end inside 64 columns.
+template <bool OUT, typename T>
+__device__ __forceinline__ void copy_tile_units(uint8_t* tile, bool narrow, uint16_t* g, long long stride, int rows, int cols, int lane) {
+    constexpr int kUnit = sizeof(T) / 2, kAcross = 64 / kUnit, kLanes = kAcross < 32 ? kAcross : 32, kDown = 32 / kLanes;
+    const int sub = lane / kLanes, first = lane % kLanes;
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            uint2 in[8];
-            float xs[8];
+    for (int part = 0; part < kAcross / kLanes; ++part) {
+        const int col = (first + part * kLanes) * kUnit;
+        if (col >= cols) continue;
+#pragma unroll 8
+        for (int r0 = 0; r0 < 32; r0 += kDown) {
+            const int r = r0 + sub;
+            T* at = reinterpret_cast<T*>(tile + place(r, col >> 3, narrow) + (col & 7) * 2);
+            if (r < rows) {
+                if (OUT) *reinterpret_cast<T*>(g + r * stride + col) = *at;
+                else *at = *reinterpret_cast<const T*>(g + r * stride + col);
+            }
+        }
+    }
+}
+template <bool OUT>
+__device__ __noinline__ void copy_tile(uint8_t* tile, bool narrow, uint16_t* g, long long stride, int rows, int cols, int lane) {
+    if (((stride | cols) & 3) == 0) copy_tile_units<OUT, unsigned long long>(tile, narrow, g, stride, rows, cols, lane);
+    else if (((stride | cols) & 1) == 0) copy_tile_units<OUT, uint32_t>(tile, narrow, g, stride, rows, cols, lane);
+    else copy_tile_units<OUT, uint16_t>(tile, narrow, g, stride, rows, cols, lane);
+}
+
+// 32 columns of a thread's row: out of TMEM (`acc`), through the epilogue, into the warp's tile from its 16-byte place `first` on.
+// IN: the places that take y hold the residual or z_in before.  Z: z goes 2 KB behind.
+template <int KIND, int ACT, bool E4M3, bool IN, bool Z>
+__device__ __forceinline__ void finish32(const uint32_t (&acc)[32], const LinearEpilogue& e, int n, int col, int first, int lane, float x_scale, uint32_t tile) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const long long row = row_a + 2 * (8 * half + i);
-                in[i] = make_uint2(0, 0);
-                xs[i] = 1.f;
-                if (in_col && row < M) {
-                    if (extra) in[i] = *reinterpret_cast<const uint2*>(extra + row * N + col);
-                    if (KIND == kLinearForward && e.x_scale) xs[i] = e.x_scale[row];
+    for (int part = 0; part < 2; ++part) {
+        float b[16], w[16];
+        if (KIND == kLinearForward) {
+            row_values(e.bias ? e.bias : g_zeros, e.bias ? col + 16 * part : 0, e.bias ? n : 64, b);
+            if (E4M3) row_values(e.w_scale, col + 16 * part, n, w);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {                  // 8 columns: one 16-byte place
+            const uint32_t at = tile + place(lane, first + 2 * part + h, Z);
+            uint32_t in[4] = {0, 0, 0, 0}, y[4], z[4];
+            if (IN) asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];\n" : "=r"(in[0]), "=r"(in[1]), "=r"(in[2]), "=r"(in[3]) : "r"(at) : "memory");
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int c = 8 * h + 2 * i, k = 16 * part + c;
+                const Pair d = pair_of(__uint_as_float(acc[k]), __uint_as_float(acc[k + 1]));
+                if (KIND == kLinearInput) {
+                    y[i] = pack2(IN ? pmul(d, act_slope2<ACT>(elems2(in[i]))) : d);
+                } else {
+                    const Pair bias = pair_of(b[c], b[c + 1]);
+                    const Pair zz = E4M3 ? pfma(d, pmul(both(x_scale), pair_of(w[c], w[c + 1])), bias) : padd(d, bias), a = act2<ACT>(zz);
+                    y[i] = pack2(IN ? padd(a, elems2(in[i])) : a);
+                    if (Z) z[i] = pack2(zz);
                 }
             }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const long long row = row_a + 2 * (8 * half + i);
-                float v[4], z[4];
-                v4(8 * half + i, v);
-                if (!in_col || row >= M) continue;
-                finish4<KIND, ACT>(v, bias, ws, xs[i], elems4(in[i]), e.w_scale != nullptr, z);
-                if (KIND == kLinearForward && e.z)
-                    *reinterpret_cast<uint2*>((uint16_t*)e.z + row * N + col) = make_uint2(pack_elem(z[0], z[1]), pack_elem(z[2], z[3]));
-                *reinterpret_cast<uint2*>((uint16_t*)e.y + row * N + col) = make_uint2(pack_elem(v[0], v[1]), pack_elem(v[2], v[3]));
-            }
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(at), "r"(y[0]), "r"(y[1]), "r"(y[2]), "r"(y[3]) : "memory");
+            if (KIND == kLinearForward && Z)
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(at + kTile / 2), "r"(z[0]), "r"(z[1]), "r"(z[2]), "r"(z[3]) : "memory");
         }
-        return;
-    }
-    // rows that are not multiples of 8 bytes
-    float b[4] = {0.f, 0.f, 0.f, 0.f}, w[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int c = 0; c < 4; ++c)
-        if (in_col && col + c < N && KIND == kLinearForward) {
-            if (e.bias) b[c] = e.bias[col + c];
-            if (e.w_scale) w[c] = e.w_scale[col + c];
-        }
-    bias = make_float4(b[0], b[1], b[2], b[3]);
-    ws = make_float4(w[0], w[1], w[2], w[3]);
-#pragma unroll 4
-    for (int i = 0; i < 16; ++i) {
-        const long long row = row_a + 2 * i;
-        float v[4], z[4], t[4] = {0.f, 0.f, 0.f, 0.f};
-        v4(i, v);
-        if (!in_col || row >= M) continue;
-        if (extra)
-#pragma unroll
-            for (int c = 0; c < 4; ++c)
-                if (col + c < N) t[c] = elem2_to_float2(extra[row * N + col + c]).x;
-        finish4<KIND, ACT>(v, bias, ws, KIND == kLinearForward && e.x_scale ? e.x_scale[row] : 1.f, make_float4(t[0], t[1], t[2], t[3]), e.w_scale != nullptr, z);
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-            if (col + c < N) {
-                if (KIND == kLinearForward && e.z) ((uint16_t*)e.z)[row * N + col + c] = (uint16_t)pack_elem(z[c], 0.f);
-                ((uint16_t*)e.y)[row * N + col + c] = (uint16_t)pack_elem(v[c], 0.f);
-            }
     }
 }
 
-// The same for sums that stay in fp32: parts of a split product, and the weight gradient
-template <class V>
-__device__ __forceinline__ void write_sums(float* out, long long M, int N, long long row0, int col0, int cols, int lane, V v4) {
-    const int j = lane & 15, col = col0 + 4 * j;
-    const long long row_a = row0 + (lane >> 4);
-    const bool in_col = 4 * j < cols && col < N;
+// Sums that stay in fp32 (parts of a split product, the weight gradient): 32 columns of a thread's row into the warp's tile, and the tile, in
+// whole rows, to global memory.  Rows of 128 bytes, places exchanged by the row's number.
+__device__ __forceinline__ void put_sums(uint32_t tile, int lane, int part, const float* v) {        // 16 columns
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const long long row = row_a + 2 * i;
+    for (int c = 0; c < 4; ++c)
+        asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};\n" ::"r"(tile + place(lane, 4 * part + c, false)), "f"(v[4 * c]), "f"(v[4 * c + 1]), "f"(v[4 * c + 2]),
+                     "f"(v[4 * c + 3]) : "memory");
+}
+__device__ __noinline__ void write_sums(uint32_t tile, float* out, long long M, int N, long long row0, int col0, int lane) {
+    const int j = lane & 7, col = col0 + 4 * j;
+    if (col >= N) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int r = 4 * i + (lane >> 3);
         float v[4];
-        v4(i, v);
-        if (!in_col || row >= M) continue;
-        float* p = out + row * N + col;
+        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];\n" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(tile + place(r, j, false)) : "memory");
+        if (row0 + r >= M) continue;
+        float* p = out + (row0 + r) * N + col;
         if ((N & 3) == 0) {
             *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
         } else {
@@ -249,8 +299,10 @@ __device__ __forceinline__ void write_sums(float* out, long long M, int N, long 
 }
 
 template <bool PAIR, int KIND, bool E4M3>
-__global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Job job) {
+__global__ void __launch_bounds__(Roles<KIND>::kThreads, 1) linear_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Job job) {
     constexpr int CTAS = PAIR ? 2 : 1;
+    using R = Roles<KIND>;
+    constexpr int kEpiWarps = R::kEpiWarps, kGroups = R::kGroups;
     constexpr int kTileRows = 128 * CTAS;
     constexpr bool A_MN = KIND == kLinearWeights, B_MN = KIND != kLinearForward;
     constexpr int kBK = E4M3 ? 128 : 64;               // elements of a stage along k
@@ -270,6 +322,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_consta
             mbar_init(bar(kBAccFull + b), 1);
             mbar_init(bar(kBAccEmpty + b), kEpiWarps * CTAS);
         }
+        for (int w = 0; w < kEpiWarps; ++w) mbar_init(bar(kBIn + w), 1);
         *cta_abort = 0;
         fence_barrier_init();
     }
@@ -290,22 +343,23 @@ __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_consta
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smem + kOffTmem);
     wait_for_prerequisites();
 
-    const long long units = (long long)job.m_tiles * job.n_tiles * job.splits;
-    const long long first = blockIdx.x / CTAS, step = gridDim.x / CTAS;
+    Units at(job, blockIdx.x / CTAS, gridDim.x / CTAS);
+    at.settle();
+    if (warp < kEpiWarp0) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(R::kRegsOther));
+    // (Warps 0 and 1 run their loops as whole warps and elect a thread for the instructions alone: what the loops count stays in the uniform
+    // registers that those instructions take their operands from.  By one thread, a stage's products took 500 cycles to issue.)
     if (warp == 0) {
-        if (lane == 0) {
-            const int cols = job.bn / CTAS;            // this CTA's share of B
-            const uint32_t bytes = CTAS * (kOperand + job.bytes_b);
-            uint32_t it = 0;
-            bool ok = true;
-            for (long long u = first; u < units && ok; u += step) {
-                const Unit x = unit_at(job, u, kTileRows);
-                const int m = (int)x.m0 + 128 * (int)rank, n = x.n0 + cols * (int)rank;
-                for (int kb = x.k0; kb < x.k1 && ok; ++kb, ++it) {
-                    const uint32_t s = it % kStages, use = it / kStages;
-                    ok = mbar_wait<0>(bar(kBEmpty + s), (use & 1) ^ 1u, cta_abort);
-                    if (!ok) break;
-                    const uint32_t full = PAIR ? leaders(bar(kBFull + s)) : bar(kBFull + s), a = base + s * 2 * kOperand, b = a + kOperand;
+        const int cols = job.bn / CTAS;                // this CTA's share of B
+        const uint32_t bytes = CTAS * (kOperand + job.bytes_b);
+        uint32_t s = 0, phase = 1, it = 0;
+        bool ok = true;
+        for (; at.there() && ok; at.next()) {
+            const int m = (int)at.m0(kTileRows) + 128 * (int)rank, n = at.n0() + cols * (int)rank, k1 = at.k1();
+            for (int kb = at.k0(); kb < k1; ++kb, ++it) {
+                ok = mbar_wait_all(bar(kBEmpty + s), phase, cta_abort);
+                if (!ok) break;
+                const uint32_t full = PAIR ? leaders(bar(kBFull + s)) : bar(kBFull + s), a = base + s * 2 * kOperand, b = a + kOperand;
+                if (elect_one()) {
                     if (rank == 0) mbar_arrive_expect_tx(bar(kBFull + s), bytes);
                     if (A_MN) {
                         load_box<PAIR>(a, &maps.a, m, kb * kBK, full);
@@ -314,163 +368,250 @@ __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_consta
                         load_box<PAIR>(a, &maps.a, kb * kBK, m, full);
                     }
                     if (B_MN) {
-                        for (int i = 0; i < job.boxes_b; ++i) load_box<PAIR>(b + i * (kOperand / 2), &maps.b, n + 64 * i, kb * kBK, full);
+                        load_box<PAIR>(b, &maps.b, n, kb * kBK, full);
+                        if (job.boxes_b > 1) load_box<PAIR>(b + kOperand / 2, &maps.b, n + 64, kb * kBK, full);
                     } else {
                         load_box<PAIR>(b, &maps.b, kb * kBK, n, full);
                     }
                 }
+                __syncwarp();
+                if (++s == kStages) { s = 0; phase ^= 1; }
             }
-            // after an expired wait: the copies in flight are waited for, so that none lands in memory that is no longer this CTA's
-            if (!ok && rank == 0) {
-                volatile int ignore = 0;
-                for (uint32_t i = it > kStages ? it - kStages : 0; i < it; ++i)
-                    mbar_wait<0>(bar(kBFull + i % kStages), (i / kStages) & 1, &ignore, 200000000LL);
-            }
+        }
+        // after an expired wait: the copies in flight are waited for, so that none lands in memory that is no longer this CTA's
+        if (!ok && rank == 0 && lane == 0) {
+            volatile int ignore = 0;
+            for (uint32_t i = it > kStages ? it - kStages : 0; i < it; ++i)
+                mbar_wait<0>(bar(kBFull + i % kStages), (i / kStages) & 1, &ignore, 200000000LL);
         }
         __syncwarp();
     } else if (warp == 1) {
-        if (rank == 0 && lane == 0) {
-            uint32_t it = 0, done = 0;
+        if (rank == 0) {
+            // 32 bytes along k a step, 16 rows of 128 bytes where k is the slow axis
+            const uint64_t da = make_sdesc_sw128(base, A_MN ? kOperand / 2 : 16), db = make_sdesc_sw128(base + kOperand, B_MN ? kOperand / 2 : 16);
+            const uint32_t hi = sdesc_hi(da), a0 = sdesc_lo(da), b0 = sdesc_lo(db);
+            constexpr uint32_t kStageLo = 2 * kOperand / 16, kALo = A_MN ? 2048 / 16 : 2, kBLo = B_MN ? 2048 / 16 : 2;
+            uint32_t s = 0, phase = 0, done = 0;
             bool ok = true;
-            for (long long u = first; u < units && ok; u += step) {
-                const Unit x = unit_at(job, u, kTileRows);
-                for (int kb = x.k0; kb < x.k1 && ok;) {
-                    const int end = KIND == kLinearWeights ? min(x.k1, kb + kLinearChunk) : x.k1;
+            for (; at.there() && ok; at.next()) {
+                const int k1 = at.k1();
+                for (int kb = at.k0(); kb < k1 && ok;) {
+                    const int end = KIND == kLinearWeights ? min(k1, kb + kLinearChunk) : k1;
                     const uint32_t buf = done & 1, acc = tmem + buf * kAccCols;
-                    ok = mbar_wait<0>(bar(kBAccEmpty + buf), ((done >> 1) & 1) ^ 1u, cta_abort);
+                    ok = mbar_wait_all(bar(kBAccEmpty + buf), ((done >> 1) & 1) ^ 1u, cta_abort);
                     if (!ok) break;
                     tc_fence_after();
                     uint32_t accumulate = 0;
-                    for (; kb < end; ++kb, ++it) {
-                        const uint32_t s = it % kStages;
-                        ok = mbar_wait<0>(bar(kBFull + s), (it / kStages) & 1, cta_abort);
+                    for (; kb < end; ++kb) {
+                        ok = mbar_wait_all(bar(kBFull + s), phase, cta_abort);
                         if (!ok) break;
                         tc_fence_after();
-                        const uint32_t a = base + s * 2 * kOperand, b = a + kOperand;
-                        // 32 bytes along k a step, 16 rows of 128 bytes where k is the slow axis
-                        const uint64_t da = make_sdesc_sw128(a, A_MN ? kOperand / 2 : 16), db = make_sdesc_sw128(b, B_MN ? kOperand / 2 : 16);
+                        const uint32_t a = a0 + s * kStageLo, b = b0 + s * kStageLo;
+                        if (elect_one()) {
+                            mma<PAIR, E4M3>(acc, a, b, hi, job.idesc, accumulate);
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            mma<PAIR, E4M3>(acc, da + k * (A_MN ? 2048 / 16 : 2), db + k * (B_MN ? 2048 / 16 : 2), job.idesc, accumulate);
-                            accumulate = 1;
+                            for (int k = 1; k < 4; ++k) mma<PAIR, E4M3>(acc, a + k * kALo, b + k * kBLo, hi, job.idesc, 1);
+                            commit<PAIR>(bar(kBEmpty + s));
                         }
-                        commit<PAIR>(bar(kBEmpty + s));
+                        __syncwarp();
+                        accumulate = 1;
+                        if (++s == kStages) { s = 0; phase ^= 1; }
                     }
                     if (!ok) break;
-                    commit<PAIR>(bar(kBAccFull + buf));
+                    if (elect_one()) commit<PAIR>(bar(kBAccFull + buf));
+                    __syncwarp();
                     ++done;
                 }
             }
         }
         __syncwarp();
     } else if (warp >= kEpiWarp0) {
-        const int quarter = warp & 3, half = (warp - kEpiWarp0) >> 2;
-        uint8_t* turn = smem + kOffTurn + (warp - kEpiWarp0) * kTurn;
-        const uint32_t turn_a = smem_u32(turn);
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(R::kRegsEpi));
+        // A chunk is 64 columns of the warp's 32 rows.  The chunks of all tiles go to the groups of four warps in turn: a warp has one or two of a tile,
+        // or none of a narrow one.  (Every warp waits for every accumulator and gives it back, so that none falls behind by a phase.)
+        const int quarter = warp & 3, group = (warp - kEpiWarp0) >> 2, chunks = (job.bn + 63) >> 6;
+        uint8_t* tile_p = smem + kOffTiles + (warp - kEpiWarp0) * kTile;
+        const uint32_t tile = smem_u32(tile_p);
         const uint32_t lane_tmem = tmem + ((uint32_t)(quarter * 32) << 16);
-        // this thread's row, 16 columns from 16 part on; the 16-byte places of a row are exchanged by the row's number against bank conflicts
-        auto put16 = [&](int part, const float* v) {
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const uint32_t at = turn_a + lane * 256 + (((4 * part + c) ^ (lane & 7)) << 4);
-                asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};\n" ::"r"(at), "f"(v[4 * c]), "f"(v[4 * c + 1]), "f"(v[4 * c + 2]), "f"(v[4 * c + 3]) : "memory");
-            }
-        };
-        auto get4 = [&](int i, float (&v)[4]) {
-            const int r = 2 * i + (lane >> 4);
-            const uint32_t at = turn_a + r * 256 + (((lane & 15) ^ (r & 7)) << 4);
-            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];\n" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(at) : "memory");
-        };
         uint32_t done = 0;
         bool ok = true;
-        for (long long u = first; u < units && ok; u += step) {
-            const Unit x = unit_at(job, u, kTileRows);
-            const long long row0 = x.m0 + 128 * rank + 32 * quarter;
-            float* sums = job.e.sums ? job.e.sums + (size_t)x.split * job.M * job.N : nullptr;
-            if constexpr (KIND == kLinearWeights) {
-                float acc[2][64];
+        int first_chunk = group;                       // of this tile's, this group's first: the tiles' chunks are counted through
+        auto next_chunk = [&] {
+            first_chunk -= chunks;
+            while (first_chunk < 0) first_chunk += kGroups;
+        };
+        auto give_back = [&](uint32_t buf) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) arrive_leader<PAIR>(bar(kBAccEmpty + buf));
+        };
+        if constexpr (KIND == kLinearWeights) {
+            for (; at.there() && ok; at.next(), next_chunk()) {
+                const long long row0 = at.m0(kTileRows) + 128 * rank + 32 * quarter;
+                const int n0 = at.n0(), k1 = at.k1();
+                const int chunk = first_chunk, col0 = 64 * chunk;          // (as many groups as chunks: a group has one at most)
+                float acc[64];
 #pragma unroll
-                for (int i = 0; i < 64; ++i) acc[0][i] = acc[1][i] = 0.f;
-                for (int kb = x.k0; kb < x.k1 && ok; kb += kLinearChunk, ++done) {
+                for (int i = 0; i < 64; ++i) acc[i] = 0.f;
+                for (int kb = at.k0(); kb < k1 && ok; kb += kLinearChunk, ++done) {
                     const uint32_t buf = done & 1;
                     ok = mbar_wait_all(bar(kBAccFull + buf), (done >> 1) & 1, cta_abort);
                     if (!ok) break;
                     tc_fence_after();
+                    if (chunk < chunks)
 #pragma unroll
-                    for (int c = 0; c < 2; ++c)
-#pragma unroll
-                        for (int p = 0; p < 4; ++p) {
-                            const int col = 64 * (2 * c + half) + 16 * p;
-                            if (col < job.bn) {
+                        for (int p = 0; p < 4; ++p)
+                            if (col0 + 16 * p < job.bn) {
                                 uint32_t t[16];
-                                tmem_ld16(lane_tmem + buf * kAccCols + col, t);
+                                tmem_ld16(lane_tmem + buf * kAccCols + col0 + 16 * p, t);
                                 tmem_ld_wait();
 #pragma unroll
-                                for (int i = 0; i < 16; ++i) acc[c][16 * p + i] += __uint_as_float(t[i]);
+                                for (int i = 0; i < 16; ++i) acc[16 * p + i] += __uint_as_float(t[i]);
                             }
-                        }
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) arrive_leader<PAIR>(bar(kBAccEmpty + buf));
+                    give_back(buf);
                 }
-                if (!ok) break;
+                if (!ok || chunk >= chunks) continue;
+                float* sums = job.e.sums + (size_t)at.at.split * job.M * job.N;
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    const int col0 = 64 * (2 * c + half);
-                    if (col0 < job.bn) {
-#pragma unroll
-                        for (int p = 0; p < 4; ++p) put16(p, &acc[c][16 * p]);
+                for (int h = 0; h < 2; ++h)
+                    if (col0 + 32 * h < job.bn) {
+                        put_sums(tile, lane, 0, &acc[32 * h]);
+                        put_sums(tile, lane, 1, &acc[32 * h + 16]);
                         __syncwarp();
-                        write_sums(sums, job.M, job.N, row0, x.n0 + col0, min(64, job.bn - col0), lane, get4);
+                        write_sums(tile, sums, job.M, job.N, row0, n0 + col0 + 32 * h, lane);
                         __syncwarp();
                     }
-                }
-            } else {
+            }
+        } else if (job.e.sums) {
+            for (; at.there() && ok; at.next(), ++done) {        // parts of a split sum
+                const long long row0 = at.m0(kTileRows) + 128 * rank + 32 * quarter;
+                const int n0 = at.n0();
                 const uint32_t buf = done & 1;
                 ok = mbar_wait_all(bar(kBAccFull + buf), (done >> 1) & 1, cta_abort);
                 if (!ok) break;
                 tc_fence_after();
-                ++done;
-                for (int col0 = 64 * half; col0 < job.bn; col0 += 128) {
-                    const int cols = min(64, job.bn - col0);
-                    uint32_t t[32];
-                    tmem_ld32(lane_tmem + buf * kAccCols + col0, t);
-                    tmem_ld_wait();
-#pragma unroll
-                    for (int p = 0; p < 2; ++p) {
-                        float f[16];
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) f[i] = __uint_as_float(t[16 * p + i]);
-                        put16(p, f);
-                    }
-                    if (cols > 32) {
-                        tmem_ld32(lane_tmem + buf * kAccCols + col0 + 32, t);
-                        tmem_ld_wait();
+                for (int chunk = first_chunk; chunk < chunks; chunk += kGroups) {
+#pragma unroll 1
+                    for (int c = 64 * chunk; c < min(job.bn, 64 * chunk + 64); c += 32) {
 #pragma unroll
                         for (int p = 0; p < 2; ++p) {
+                            uint32_t t[16];
                             float f[16];
+                            tmem_ld16(lane_tmem + buf * kAccCols + c + 16 * p, t);
+                            tmem_ld_wait();
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) f[i] = __uint_as_float(t[16 * p + i]);
-                            put16(2 + p, f);
+                            for (int i = 0; i < 16; ++i) f[i] = __uint_as_float(t[i]);
+                            put_sums(tile, lane, p, f);
+                        }
+                        __syncwarp();
+                        write_sums(tile, job.e.sums + (size_t)at.at.split * job.M * job.N, job.M, job.N, row0, n0 + c, lane);
+                        __syncwarp();
+                    }
+                }
+                give_back(buf);
+                next_chunk();
+            }
+        } else {
+            // The tile takes the residual (or z_in) first and y over it, each thread its row.  With z a chunk goes in two pieces of 32 columns, y in the
+            // first 2 KB of the tile and z in the others.
+            const void* in = KIND == kLinearForward ? job.e.residual : job.e.z_in;
+            const bool has_in = in != nullptr, has_z = KIND == kLinearForward && !E4M3 && job.e.z != nullptr;
+            const int width = has_z ? 32 : 64;
+            const uint32_t in_bar = bar(kBIn + warp - kEpiWarp0);
+            uint32_t n_in = 0;                         // tiles that the copy engine brought
+            for (; at.there() && ok; at.next(), ++done) {
+                const long long row0 = at.m0(kTileRows) + 128 * rank + 32 * quarter;
+                const int n0 = at.n0();
+                const uint32_t buf = done & 1, acc = lane_tmem + buf * kAccCols;
+                const int rows = (int)min(32ll, job.M - row0);
+                // (rows <= 0: the tile's last rows are no rows)
+                const bool fetched = has_in && job.by_map;
+                auto prepare = [&](int col) {          // by one lane
+                    stores_read<0>();                  // the tile is free
+                    if (fetched) {
+                        mbar_arrive_expect_tx(in_bar, 64 * width);
+                        tma_load_2d(tile, &maps.in, col, (int)row0, in_bar);
+                    }
+                };
+                bool mine = false;                     // the residual comes while the accumulator is waited for
+                if (first_chunk < chunks && rows > 0 && n0 + 64 * first_chunk < job.N) {
+                    mine = true;
+                    if (lane == 0) prepare(n0 + 64 * first_chunk);
+                }
+                ok = mbar_wait_all(bar(kBAccFull + buf), (done >> 1) & 1, cta_abort);
+                if (!ok) {
+                    if (mine && fetched && lane == 0) {       // it lands before this CTA ends
+                        volatile int ignore = 0;
+                        mbar_wait<0>(in_bar, n_in & 1, &ignore, 200000000LL);
+                    }
+                    break;
+                }
+                tc_fence_after();
+                bool given = false;
+                if (const int chunk = first_chunk; mine) {       // (as many groups as chunks: a group has one at most)
+                    const int col0 = 64 * chunk, col = n0 + col0, cols = min(64, job.bn - col0), own = min(cols, job.N - col);
+                    uint32_t cur[32];
+                    tmem_ld32(acc + col0, cur);
+                    const bool engine = job.by_map && (has_z || cols == 64 || col + cols >= job.N);     // else the tile's last columns are a neighbour's
+                    float x_scale = 1.f;
+                    if (E4M3 && lane < rows) x_scale = __ldg(job.e.x_scale + row0 + lane);
+#pragma unroll 1
+                    for (int p0 = 0; p0 < cols; p0 += 32) {
+                        if (p0 > 0) tmem_ld32(acc + col0 + p0, cur);
+                        if (p0 == 0 || has_z) {        // a new tile
+                            if (lane == 0 && p0 > 0) prepare(col + p0);
+                            __syncwarp();
+                            if (fetched) {
+                                ok = mbar_wait_all(in_bar, n_in & 1, cta_abort);
+                                if (!ok) {
+                                    volatile int ignore = 0;
+                                    if (lane == 0) mbar_wait<0>(in_bar, n_in & 1, &ignore, 200000000LL);
+                                    break;
+                                }
+                                ++n_in;
+                            } else if (has_in) {
+                                if (own > p0) copy_tile<false>(tile_p, has_z, (uint16_t*)in + row0 * job.N + col + p0, job.N, rows, min(width, own - p0), lane);
+                                __syncwarp();
+                            }
+                        }
+                        tmem_ld_wait();
+                        if (p0 + 32 >= cols) {         // the accumulator has been read
+                            give_back(buf);
+                            given = true;
+                        }
+                        with_act(job.e.activation, [&](auto tag) {
+                            constexpr int ACT = decltype(tag)::value;
+                            if (has_z && has_in) finish32<KIND, ACT, E4M3, true, true>(cur, job.e, job.N, col + p0, 0, lane, x_scale, tile);
+                            else if (has_z) finish32<KIND, ACT, E4M3, false, true>(cur, job.e, job.N, col + p0, 0, lane, x_scale, tile);
+                            else if (has_in) finish32<KIND, ACT, E4M3, true, false>(cur, job.e, job.N, col + p0, p0 >> 3, lane, x_scale, tile);
+                            else finish32<KIND, ACT, E4M3, false, false>(cur, job.e, job.N, col + p0, p0 >> 3, lane, x_scale, tile);
+                        });
+                        if (!has_z && p0 + 32 < cols) continue;
+                        const int at = has_z ? p0 : 0; // the tile's first column
+                        if (engine) {
+                            fence_proxy_async();
+                            __syncwarp();
+                            if (lane == 0) {
+                                store_box(&maps.y, col + at, (int)row0, tile);
+                                if (has_z) store_box(&maps.z, col + at, (int)row0, tile + kTile / 2);
+                                stores_commit();
+                            }
+                        } else {
+                            __syncwarp();
+                            if (own > at) {
+                                const long long where = row0 * job.N + col + at;
+                                copy_tile<true>(tile_p, has_z, (uint16_t*)job.e.y + where, job.N, rows, min(width, own - at), lane);
+                                if (has_z) copy_tile<true>(tile_p + kTile / 2, true, (uint16_t*)job.e.z + where, job.N, rows, min(width, own - at), lane);
+                            }
+                            __syncwarp();
                         }
                     }
-                    if (col0 + 128 >= job.bn) {        // the accumulator has been read
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) arrive_leader<PAIR>(bar(kBAccEmpty + buf));
-                    }
-                    __syncwarp();
-                    if (sums) {
-                        write_sums(sums, job.M, job.N, row0, x.n0 + col0, cols, lane, get4);
-                    } else {
-                        with_act(job.e.activation, [&](auto tag) {
-                            write_rows<KIND, decltype(tag)::value>(job.e, job.M, job.N, row0, x.n0 + col0, cols, lane, get4);
-                        });
-                    }
-                    __syncwarp();
                 }
-                if (64 * half >= job.bn && lane == 0) arrive_leader<PAIR>(bar(kBAccEmpty + buf));      // a narrow tile has no columns for this warp
+                if (ok && !given) give_back(buf);      // a warp without a chunk here, or whose last one has no rows or columns
+                next_chunk();
             }
+            if (lane == 0) stores_read<0>();
+            __syncwarp();
         }
     }
 
@@ -528,9 +669,18 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const LinearEpilogue e
             w[c] = in && KIND == kLinearForward && e.w_scale ? e.w_scale[col + c] : 0.f;
             t[c] = in && extra ? elem2_to_float2(extra[at + c]).x : 0.f;
         }
+        const bool scaled = KIND == kLinearForward && e.x_scale;
+        const Pair xs = both(scaled ? e.x_scale[row] : 1.f);
         with_act(e.activation, [&](auto tag) {
-            finish4<KIND, decltype(tag)::value>(v, make_float4(b[0], b[1], b[2], b[3]), make_float4(w[0], w[1], w[2], w[3]),
-                                                KIND == kLinearForward && e.x_scale ? e.x_scale[row] : 1.f, make_float4(t[0], t[1], t[2], t[3]), e.w_scale != nullptr, z);
+#pragma unroll
+            for (int c = 0; c < 4; c += 2) {
+                Pair zz = 0, y;
+                const Pair d = pair_of(v[c], v[c + 1]), bb = pair_of(b[c], b[c + 1]), in = pair_of(t[c], t[c + 1]);
+                if (scaled) y = finish2<KIND, decltype(tag)::value, true>(d, bb, pmul(xs, pair_of(w[c], w[c + 1])), in, zz);
+                else y = finish2<KIND, decltype(tag)::value, false>(d, bb, 0, in, zz);
+                split_pair(y, v[c], v[c + 1]);
+                split_pair(zz, z[c], z[c + 1]);
+            }
         });
         if (wide) {
             if (KIND == kLinearForward && e.z) *reinterpret_cast<uint2*>((uint16_t*)e.z + at) = make_uint2(pack_elem(z[0], z[1]), pack_elem(z[2], z[3]));
@@ -561,16 +711,16 @@ EncodeTiledFn encode_tiled_fn() {
     return fn;
 }
 
-// [slow][fast] with rows of `stride` bytes, boxes of 128 bytes x box_rows; beyond the tensor zeros are read
-bool encode_map(CUtensorMap* map, const void* base, long long fast, long long slow, long long stride, int elem_bytes, int box_rows) {
+// [slow][fast] with rows of `stride` bytes, boxes of box_bytes (128 or 64, swizzled over as many) x box_rows; beyond the tensor zeros are read
+bool encode_map(CUtensorMap* map, const void* base, long long fast, long long slow, long long stride, int elem_bytes, int box_rows, int box_bytes = 128) {
     EncodeTiledFn enc = encode_tiled_fn();
     if (!enc) return false;
     const cuuint64_t dims[2] = {(cuuint64_t)fast, (cuuint64_t)slow};
     const cuuint64_t strides[1] = {(cuuint64_t)stride};
-    const cuuint32_t box[2] = {(cuuint32_t)(128 / elem_bytes), (cuuint32_t)box_rows};
+    const cuuint32_t box[2] = {(cuuint32_t)(box_bytes / elem_bytes), (cuuint32_t)box_rows};
     const cuuint32_t estr[2] = {1u, 1u};
     return enc(map, elem_bytes == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr,
-               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+               CU_TENSOR_MAP_INTERLEAVE_NONE, box_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 template <bool PAIR, int KIND, bool E4M3>
@@ -578,7 +728,7 @@ cudaError_t launch_one(const Maps& maps, const Job& job, int sm_count, cudaStrea
     auto kern = linear_kernel<PAIR, KIND, E4M3>;
     cudaError_t e = prepare_kernel((const void*)kern, kSmem);
     if (e != cudaSuccess) return e;
-    const long long units = (long long)job.m_tiles * job.n_tiles * job.splits, fit = sm_count / (PAIR ? 2 : 1);
+    const unsigned units = (unsigned)(job.groups * job.group * job.n_tiles * job.splits), fit = (unsigned)sm_count / (PAIR ? 2 : 1);
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -586,8 +736,8 @@ cudaError_t launch_one(const Maps& maps, const Job& job, int sm_count, cudaStrea
     attr[1].val.clusterDim.x = PAIR ? 2 : 1;
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(units < fit ? units : fit) * (PAIR ? 2 : 1));
-    cfg.blockDim = dim3(kThreads);
+    cfg.gridDim = dim3((units < fit ? units : fit) * (PAIR ? 2 : 1));
+    cfg.blockDim = dim3(Roles<KIND>::kThreads);
     cfg.dynamicSmemBytes = kSmem;
     cfg.stream = stream;
     cfg.attrs = attr;
@@ -617,20 +767,30 @@ cudaError_t launch_linear(int kind, bool e4m3, const LinearPlan& p, long long M,
     if (!encode_map(&maps.a, a, a_mn ? M : K, a_mn ? K : M, stride_a, elem, a_mn ? 64 : 128) ||
         !encode_map(&maps.b, b, b_mn ? N : K, b_mn ? K : N, stride_b, elem, b_mn ? 64 : cols))
         return cudaErrorInvalidValue;
-    Job job;
+    const void* in = kind == kLinearForward ? epi.residual : epi.z_in;
+    const bool by_map = kind != kLinearWeights && p.splits == 1 && N % 8 == 0;
+    maps.in = maps.y = maps.z = maps.a;
+    const int wide = epi.z ? 64 : 128;
+    if (by_map && ((in && !encode_map(&maps.in, in, N, M, 2ll * N, 2, 32, wide)) || !encode_map(&maps.y, epi.y, N, M, 2ll * N, 2, 32, wide) ||
+                   (epi.z && !encode_map(&maps.z, epi.z, N, M, 2ll * N, 2, 32, wide))))
+        return cudaErrorInvalidValue;
+    Job job = {};
     job.M = M;
     job.N = N;
     job.bn = p.bn;
     job.m_tiles = p.m_tiles;
     job.n_tiles = p.n_tiles;
-    job.group = p.group;
+    job.group = p.group < p.m_tiles ? p.group : p.m_tiles;
+    job.groups = (p.m_tiles + job.group - 1) / job.group;
     job.splits = p.splits;
     job.k_blocks = p.k_blocks;
     job.kb_per_split = p.kb_per_split;
+    if ((long long)job.groups * job.group * p.n_tiles * p.splits > 0x3fffffffLL) return cudaErrorInvalidConfiguration;
     job.boxes_b = (cols + 63) / 64;
     job.bytes_b = b_mn ? job.boxes_b * (kOperand / 2) : cols * 128;
     job.idesc = e4m3 ? make_idesc_f16(128 * ctas, p.bn, 0, 0)            // e4m3 has format number 0, as fp16 has in its kind
                      : make_idesc_elem(128 * ctas, p.bn, a_mn ? 1 : 0, b_mn ? 1 : 0);
+    job.by_map = by_map;
     job.e = epi;
     job.e.sums = p.splits > 1 ? parts : kind == kLinearWeights ? out : nullptr;
     cudaError_t e;

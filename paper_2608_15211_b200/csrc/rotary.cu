@@ -20,16 +20,6 @@ constexpr int kBlock = 256;
 constexpr int kMaxTokens = 64, kMaxAngles = 2048;     // of a block
 constexpr int kMaxHeads = 128;                        // of a block: more go to other blocks
 
-// n / d for n d < 2^32, by a multiplication
-struct Divider {
-    uint32_t d, m;
-    __host__ explicit Divider(uint32_t by) : d(by), m(by > 1 ? (uint32_t)(0x100000000ull / by) + 1 : 0) {}
-    __device__ void split(uint32_t n, uint32_t& quo, uint32_t& rem) const {
-        quo = d > 1 ? __umulhi(n, m) : n;
-        rem = n - quo * d;
-    }
-};
-
 template <int E> struct Words;                        // E elements as they lie in memory
 template <> struct Words<8> { uint4 v; };
 template <> struct Words<2> { uint32_t v; };
@@ -168,7 +158,6 @@ cudaError_t launch_rotary(const RotaryArgs& a, int sm_count, cudaStream_t stream
     if (tokens > kMaxTokens) tokens = kMaxTokens;
     if (tokens > kMaxAngles / pairs) tokens = kMaxAngles / pairs;
     if (tokens < 1) tokens = 1;
-    // (a block's items, tokens x per_token, are below 2^15 + 2^11: what Divider asks for)
     const Deal deal{(int)tokens, heads, turned, turned + copied, tensors, Divider((uint32_t)per_token), Divider((uint32_t)(turned + copied)),
                     Divider((uint32_t)pairs)};
     const long long blocks = (a.tokens + tokens - 1) / tokens;
