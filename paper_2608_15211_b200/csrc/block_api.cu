@@ -68,10 +68,15 @@ struct LinearLayout {
     size_t bytes;
 };
 
+// Few rows on the plain arithmetic units / on the tensor cores, us: 1 x 4096 -> 4096 4.9 / 12.4, 2 x 4096 -> 8192 10.2 / 20.3, 4 rows 16.4 / 20.5, 8 rows
+// 30.2 / 20.7, but 8 x 1024 -> 1024 3.2 / 8.5: a launch and a tile's latency against an arithmetic that grows with the rows.
+bool few_rows(const terra_linear_desc* d) { return d->rows <= 4 || (d->rows <= kFewRows && (long long)d->n_in * d->n_out <= 12000000); }
+
 LinearLayout layout_linear(const terra_linear_desc* d, int call) {
     LinearLayout l = {};
     LinearSpace s;
     const bool e4m3 = call == TERRA_LINEAR_FWD_E4M3, bwd = call == TERRA_LINEAR_BWD;
+    if (!bwd && few_rows(d)) return l;
     const long long elem = e4m3 ? 1 : 2;
     l.stride_x = l.stride_w = padded(d->n_in * elem);
     l.stride_z = padded(d->n_out * elem);
@@ -121,13 +126,17 @@ int linear_fwd(const terra_linear_desc* d, bool e4m3, const void* x, const float
     char* ws = (char*)workspace;
     cudaStream_t st = (cudaStream_t)stream;
     const long long elem = e4m3 ? 1 : 2;
-    cudaError_t e = pad(x, l.pad_x, ws + l.off_x, d->rows, d->n_in * elem, l.stride_x, sms, st);
-    if (e == cudaSuccess) e = pad(w, l.pad_w, ws + l.off_w, d->n_out, d->n_in * elem, l.stride_w, sms, st);
-    if (e != cudaSuccess) return done(e, where);
     LinearEpilogue epi = {};
     epi.bias = bias; epi.residual = residual; epi.y = y; epi.z = z; epi.activation = d->activation;
     epi.x_scale = e4m3 ? x_scale : nullptr;
     epi.w_scale = e4m3 ? w_scale : nullptr;
+    if (few_rows(d)) {
+        auto few = d->dtype == TERRA_DTYPE_F16 ? launch_linear_few_f16 : launch_linear_few;
+        return done(few(e4m3, (int)d->rows, d->n_in, d->n_out, x, w, epi, st), where);
+    }
+    cudaError_t e = pad(x, l.pad_x, ws + l.off_x, d->rows, d->n_in * elem, l.stride_x, sms, st);
+    if (e == cudaSuccess) e = pad(w, l.pad_w, ws + l.off_w, d->n_out, d->n_in * elem, l.stride_w, sms, st);
+    if (e != cudaSuccess) return done(e, where);
     auto launch = d->dtype == TERRA_DTYPE_F16 ? launch_linear_f16 : launch_linear;
     return done(launch(kLinearForward, e4m3, l.first, d->rows, d->n_out, d->n_in, x, l.stride_x, w, l.stride_w, epi, nullptr, (float*)(ws + l.off_parts), sms, st), where);
 }
@@ -162,7 +171,7 @@ int rotary(const terra_swin_desc* desc, const terra_rotary_desc* r, const double
 }  // namespace
 
 // The tile, and into how many parts the sum is split, by an estimate of the time in SM cycles.
-LinearPlan plan_linear(int kind, bool e4m3, long long M, int N, long long K) {
+static LinearPlan make_plan(int kind, bool e4m3, long long M, int N, long long K) {
     const long long blocks = (K + (e4m3 ? 127 : 63)) / (e4m3 ? 128 : 64);
     LinearPlan best = {};
     double best_cost = 1e300;
@@ -200,6 +209,21 @@ LinearPlan plan_linear(int kind, bool e4m3, long long M, int N, long long K) {
     }
     best.group = 8;
     return best;
+}
+
+// Each thread remembers the plans of its last few sizes: the search takes longer than a launch, and a call asks for its plans twice.
+LinearPlan plan_linear(int kind, bool e4m3, long long M, int N, long long K) {
+    struct Known { long long M = 0, K; int kind, N; bool e4m3; LinearPlan plan; };
+    constexpr int kKnown = 32;
+    static thread_local Known known[kKnown];
+    static thread_local int next = 0;
+    for (const Known& k : known)
+        if (k.M == M && k.K == K && k.N == N && k.kind == kind && k.e4m3 == e4m3) return k.plan;
+    Known& k = known[next];
+    next = (next + 1) % kKnown;
+    k.plan = make_plan(kind, e4m3, M, N, K);
+    k.M = M; k.K = K; k.N = N; k.kind = kind; k.e4m3 = e4m3;
+    return k.plan;
 }
 
 }  // namespace terra

@@ -88,6 +88,10 @@ cudaError_t launch_linear(int kind, bool e4m3, const LinearPlan& p, long long M,
                           const LinearEpilogue& epi, float* out, float* parts, int sm_count, cudaStream_t stream);
 cudaError_t launch_linear_f16(int kind, bool e4m3, const LinearPlan& p, long long M, int N, long long K, const void* a, long long stride_a, const void* b, long long stride_b,
                               const LinearEpilogue& epi, float* out, float* parts, int sm_count, cudaStream_t stream);
+// the forward product for up to kFewRows rows (linear_few.cu): rows of any length, no workspace
+constexpr int kFewRows = 8;
+cudaError_t launch_linear_few(bool e4m3, int rows, int n_in, int n_out, const void* x, const void* w, const LinearEpilogue& epi, cudaStream_t stream);
+cudaError_t launch_linear_few_f16(bool e4m3, int rows, int n_in, int n_out, const void* x, const void* w, const LinearEpilogue& epi, cudaStream_t stream);
 cudaError_t read_linear_status(int* timed_out);       // after the stream has been synchronised
 cudaError_t read_linear_status_f16(int* timed_out);
 

@@ -116,11 +116,15 @@ __device__ __forceinline__ void stores_commit() { asm volatile("cp.async.bulk.co
 template <int N>
 __device__ __forceinline__ void stores_read() { asm volatile("cp.async.bulk.wait_group.read %0;\n" ::"n"(N) : "memory"); }   // all but the last N
 
+struct Digits { int m, n, g, split; };      // of a unit's number, see Units
+
 struct Job {
     long long M;
     int N;
     int bn;                                    // columns of a tile: a multiple of 32
     int m_tiles, n_tiles, group, groups;       // tiles are walked through in groups of `group` rows of tiles
+    Divider by_group{1}, by_n_tiles{1}, by_groups{1};
+    Digits step;                               // of the number of tiles that are worked on at a time
     int splits, k_blocks, kb_per_split;
     int bytes_b;                               // of a CTA's share of B in a stage
     int boxes_b;                               // MN-major: boxes of 64 columns
@@ -132,21 +136,17 @@ struct Job {
 // A unit as digits: the row of tiles within its group (fastest), the column of tiles, the group, the part of the sum.  Going `step` units on adds the
 // step's digits with carries.  (Divisions, in every role for every tile, cost each tile 700 cycles, 64-bit ones 1500.)  The last group
 // may have fewer rows than the others: its units beyond are there and empty.
-struct Digits { int m, n, g, split; };
 __device__ __forceinline__ Digits digits_of(const Job& j, uint32_t u) {
-    Digits d;
-    d.m = (int)(u % j.group);
-    u /= j.group;
-    d.n = (int)(u % j.n_tiles);
-    u /= j.n_tiles;
-    d.g = (int)(u % j.groups);
-    d.split = (int)(u / j.groups);
-    return d;
+    uint32_t m, n, g, split;
+    j.by_group.split(u, u, m);
+    j.by_n_tiles.split(u, u, n);
+    j.by_groups.split(u, split, g);
+    return {(int)m, (int)n, (int)g, (int)split};
 }
 struct Units {
     const Job& j;
     Digits at, step;
-    __device__ __forceinline__ Units(const Job& job, uint32_t first, uint32_t by) : j(job), at(digits_of(job, first)), step(digits_of(job, by)) {}
+    __device__ __forceinline__ Units(const Job& job, uint32_t first) : j(job), at(digits_of(job, first)), step(job.step) {}
     __device__ __forceinline__ bool there() const { return at.split < j.splits; }
     __device__ __forceinline__ bool empty() const { return at.g * j.group + at.m >= j.m_tiles; }
     __device__ __forceinline__ void advance() {
@@ -183,6 +183,8 @@ __device__ __forceinline__ Pair finish2(Pair d, Pair bias, Pair scale, Pair in, 
 }
 __device__ __forceinline__ Pair elems2(uint32_t v) { const float2 t = elem2_to_float2(v); return pair_of(t.x, t.y); }
 __device__ __forceinline__ uint32_t pack2(Pair p) { float a, b; split_pair(p, a, b); return pack_elem(a, b); }
+
+__device__ __forceinline__ void prefetch_l1(const float* p) { asm volatile("prefetch.global.L1 [%0];\n" ::"l"(p)); }
 
 __device__ float g_zeros[64];          // what stands for a bias that is not there
 
@@ -343,7 +345,7 @@ __global__ void __launch_bounds__(Roles<KIND>::kThreads, 1) linear_kernel(const 
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(smem + kOffTmem);
     wait_for_prerequisites();
 
-    Units at(job, blockIdx.x / CTAS, gridDim.x / CTAS);
+    Units at(job, blockIdx.x / CTAS);
     at.settle();
     if (warp < kEpiWarp0) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(R::kRegsOther));
     // (Warps 0 and 1 run their loops as whole warps and elect a thread for the instructions alone: what the loops count stays in the uniform
@@ -536,7 +538,13 @@ __global__ void __launch_bounds__(Roles<KIND>::kThreads, 1) linear_kernel(const 
                 bool mine = false;                     // the residual comes while the accumulator is waited for
                 if (first_chunk < chunks && rows > 0 && n0 + 64 * first_chunk < job.N) {
                     mine = true;
-                    if (lane == 0) prepare(n0 + 64 * first_chunk);
+                    const int c = n0 + 64 * first_chunk;
+                    if (lane == 0) prepare(c);
+                    // (the bias of the chunk: from HBM, it took longer than the rest of a small product's epilogue)
+                    if (KIND == kLinearForward && lane < 2 && c + 32 * lane < job.N) {
+                        if (job.e.bias) prefetch_l1(job.e.bias + c + 32 * lane);
+                        if (E4M3) prefetch_l1(job.e.w_scale + c + 32 * lane);
+                    }
                 }
                 ok = mbar_wait_all(bar(kBAccFull + buf), (done >> 1) & 1, cta_abort);
                 if (!ok) {
@@ -724,11 +732,13 @@ bool encode_map(CUtensorMap* map, const void* base, long long fast, long long sl
 }
 
 template <bool PAIR, int KIND, bool E4M3>
-cudaError_t launch_one(const Maps& maps, const Job& job, int sm_count, cudaStream_t stream) {
+cudaError_t launch_one(const Maps& maps, Job& job, int sm_count, cudaStream_t stream) {
     auto kern = linear_kernel<PAIR, KIND, E4M3>;
     cudaError_t e = prepare_kernel((const void*)kern, kSmem);
     if (e != cudaSuccess) return e;
-    const unsigned units = (unsigned)(job.groups * job.group * job.n_tiles * job.splits), fit = (unsigned)sm_count / (PAIR ? 2 : 1);
+    const unsigned units = (unsigned)(job.groups * job.group * job.n_tiles * job.splits), fit = (unsigned)sm_count / (PAIR ? 2 : 1), at_a_time = units < fit ? units : fit;
+    job.step = {(int)(at_a_time % job.group), (int)(at_a_time / job.group % job.n_tiles), (int)(at_a_time / job.group / job.n_tiles % job.groups),
+                (int)(at_a_time / job.group / job.n_tiles / job.groups)};
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -736,7 +746,7 @@ cudaError_t launch_one(const Maps& maps, const Job& job, int sm_count, cudaStrea
     attr[1].val.clusterDim.x = PAIR ? 2 : 1;
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((units < fit ? units : fit) * (PAIR ? 2 : 1));
+    cfg.gridDim = dim3(at_a_time * (PAIR ? 2 : 1));
     cfg.blockDim = dim3(Roles<KIND>::kThreads);
     cfg.dynamicSmemBytes = kSmem;
     cfg.stream = stream;
@@ -774,7 +784,7 @@ cudaError_t launch_linear(int kind, bool e4m3, const LinearPlan& p, long long M,
     if (by_map && ((in && !encode_map(&maps.in, in, N, M, 2ll * N, 2, 32, wide)) || !encode_map(&maps.y, epi.y, N, M, 2ll * N, 2, 32, wide) ||
                    (epi.z && !encode_map(&maps.z, epi.z, N, M, 2ll * N, 2, 32, wide))))
         return cudaErrorInvalidValue;
-    Job job = {};
+    Job job{};
     job.M = M;
     job.N = N;
     job.bn = p.bn;
@@ -782,6 +792,9 @@ cudaError_t launch_linear(int kind, bool e4m3, const LinearPlan& p, long long M,
     job.n_tiles = p.n_tiles;
     job.group = p.group < p.m_tiles ? p.group : p.m_tiles;
     job.groups = (p.m_tiles + job.group - 1) / job.group;
+    job.by_group = Divider((uint32_t)job.group);
+    job.by_n_tiles = Divider((uint32_t)p.n_tiles);
+    job.by_groups = Divider((uint32_t)job.groups);
     job.splits = p.splits;
     job.k_blocks = p.k_blocks;
     job.kb_per_split = p.kb_per_split;

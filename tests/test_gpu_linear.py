@@ -12,7 +12,7 @@ BF16, F16, E4M3 = torch.bfloat16, torch.float16, torch.float8_e4m3fn
 ACTS = ["none", "relu", "silu", "gelu", "gelu_tanh"]
 
 # rows, n_in, n_out: one row, fewer than a tile, tiles and a bit, features that are no multiple of 8 (padded rows) or of 4 (rows of odd bytes), long sums
-SHAPES = [(1, 64, 32), (1, 8, 8), (3, 13, 5), (17, 96, 288), (128, 64, 128), (129, 200, 100), (256, 64, 256), (300, 384, 130), (513, 72, 372), (257, 1024, 514),
+SHAPES = [(1, 64, 32), (1, 8, 8), (3, 13, 5), (7, 46, 70), (8, 8192, 24), (9, 72, 40), (17, 96, 288), (128, 64, 128), (129, 200, 100), (256, 64, 256), (300, 384, 130), (513, 72, 372), (257, 1024, 514),
           (1000, 33, 31), (2048, 96, 96), (2, 4096, 1024), (5, 2048, 40), (700, 256, 744), (1500, 520, 1)]
 
 
