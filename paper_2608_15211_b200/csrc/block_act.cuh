@@ -64,6 +64,15 @@ __device__ __forceinline__ float act_slope(float z) {
     return 1.f;
 }
 
+// (lo, hi) += the two elements of v, one instruction each (sm_100)
+__device__ __forceinline__ void add_elems(float& lo, float& hi, uint32_t v) {
+#ifdef TERRA_ELEM_F16
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tadd.rn.f32.f16 %0, l, %0;\n\tadd.rn.f32.f16 %1, h, %1;\n\t}\n" : "+f"(lo), "+f"(hi) : "r"(v));
+#else
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tadd.rn.f32.bf16 %0, l, %0;\n\tadd.rn.f32.bf16 %1, h, %1;\n\t}\n" : "+f"(lo), "+f"(hi) : "r"(v));
+#endif
+}
+
 // ---- two at a time (one instruction for a pair of additions or products, sm_100) --------------------------------
 typedef unsigned long long Pair;                       // two fp32
 __device__ __forceinline__ Pair pair_of(float a, float b) { Pair p; asm("mov.b64 %0, {%1, %2};\n" : "=l"(p) : "f"(a), "f"(b)); return p; }

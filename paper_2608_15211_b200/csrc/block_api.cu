@@ -94,7 +94,8 @@ LinearLayout layout_linear(const terra_linear_desc* d, int call) {
         l.second = plan_linear(kLinearWeights, false, d->n_out, d->n_in, d->rows);
         need(l.first, (size_t)d->rows * d->n_in);
         need(l.second, (size_t)d->n_out * d->n_in);
-        l.off_sums = s.add(sizeof(float) * (size_t)column_sum_blocks(d->rows, d->n_out) * d->n_out);
+        const size_t slices = column_sum_blocks(d->rows, d->n_out), splits = l.second.splits * l.second.n_tiles;        // without or with the weight gradient
+        l.off_sums = s.add(sizeof(float) * (slices > splits ? slices : splits) * d->n_out);
     } else {
         l.first = plan_linear(kLinearForward, e4m3, d->rows, d->n_out, d->n_in);
         need(l.first, (size_t)d->rows * d->n_out);
@@ -138,7 +139,7 @@ int linear_fwd(const terra_linear_desc* d, bool e4m3, const void* x, const float
     if (e == cudaSuccess) e = pad(w, l.pad_w, ws + l.off_w, d->n_out, d->n_in * elem, l.stride_w, sms, st);
     if (e != cudaSuccess) return done(e, where);
     auto launch = d->dtype == TERRA_DTYPE_F16 ? launch_linear_f16 : launch_linear;
-    return done(launch(kLinearForward, e4m3, l.first, d->rows, d->n_out, d->n_in, x, l.stride_x, w, l.stride_w, epi, nullptr, (float*)(ws + l.off_parts), sms, st), where);
+    return done(launch(kLinearForward, e4m3, l.first, d->rows, d->n_out, d->n_in, x, l.stride_x, w, l.stride_w, epi, nullptr, (float*)(ws + l.off_parts), nullptr, sms, st), where);
 }
 
 // ---- rotary positions -------------------------------------------------------------------------------------------
@@ -300,7 +301,7 @@ int terra_linear_bwd(const terra_linear_desc* desc, const void* x, const void* w
     if (rc) return rc;
     const char* where = "terra_linear_bwd";
     char* ws = (char*)workspace;
-    float* parts = (float*)(ws + l.off_parts);
+    float *parts = (float*)(ws + l.off_parts), *sums = (float*)(ws + l.off_sums);
     cudaStream_t st = (cudaStream_t)stream;
     const bool f16 = desc->dtype == TERRA_DTYPE_F16;
     auto launch = f16 ? launch_linear_f16 : launch_linear;
@@ -308,11 +309,11 @@ int terra_linear_bwd(const terra_linear_desc* desc, const void* x, const void* w
     // (the weight gradient first: d_x may be written over z_in, which is x's neighbour in no call, but reads stay ahead of writes)
     if (e == cudaSuccess && d_w) {
         e = pad(x, l.pad_x, ws + l.off_x, desc->rows, 2ll * desc->n_in, l.stride_x, sms, st);
+        LinearEpilogue epi = {};
+        epi.a_sums = d_bias;
         if (e == cudaSuccess)
-            e = launch(kLinearWeights, false, l.second, desc->n_out, desc->n_in, desc->rows, d_z, l.stride_z, x, l.stride_x, LinearEpilogue{}, d_w, parts, sms, st);
-    }
-    if (e == cudaSuccess && d_bias) {
-        float* sums = (float*)(ws + l.off_sums);
+            e = launch(kLinearWeights, false, l.second, desc->n_out, desc->n_in, desc->rows, d_z, l.stride_z, x, l.stride_x, epi, d_w, parts, sums, sms, st);
+    } else if (e == cudaSuccess && d_bias) {
         e = f16 ? launch_column_sums_f16(d_z, desc->rows, desc->n_out, l.stride_z / 2, sums, d_bias, st)
                 : launch_column_sums(d_z, desc->rows, desc->n_out, l.stride_z / 2, sums, d_bias, st);
     }
@@ -321,7 +322,7 @@ int terra_linear_bwd(const terra_linear_desc* desc, const void* x, const void* w
         LinearEpilogue epi = {};
         epi.z_in = z_in; epi.y = d_x; epi.activation = z_in ? desc->activation : TERRA_ACT_NONE;
         if (e == cudaSuccess)
-            e = launch(kLinearInput, false, l.first, desc->rows, desc->n_in, desc->n_out, d_z, l.stride_z, w, l.stride_w, epi, nullptr, parts, sms, st);
+            e = launch(kLinearInput, false, l.first, desc->rows, desc->n_in, desc->n_out, d_z, l.stride_z, w, l.stride_w, epi, nullptr, parts, nullptr, sms, st);
     }
     return done(e, where);
 }

@@ -80,14 +80,15 @@ struct LinearEpilogue {
     const float *bias, *x_scale, *w_scale;
     const void *residual, *z_in;
     void *y, *z;
+    float* a_sums;                     // weight gradient: the sums of A(m, .) over k, that is d_z over the rows; may be NULL
     float* sums;                       // set by launch_linear
     int activation;
 };
-// `parts`: splits x M x N floats where the plan splits the sum; `out`: the weight gradient
+// `parts`: splits x M x N floats where the plan splits the sum, `a_parts` splits x n_tiles x M where a_sums is asked for too; `out`: the weight gradient
 cudaError_t launch_linear(int kind, bool e4m3, const LinearPlan& p, long long M, int N, long long K, const void* a, long long stride_a, const void* b, long long stride_b,
-                          const LinearEpilogue& epi, float* out, float* parts, int sm_count, cudaStream_t stream);
+                          const LinearEpilogue& epi, float* out, float* parts, float* a_parts, int sm_count, cudaStream_t stream);
 cudaError_t launch_linear_f16(int kind, bool e4m3, const LinearPlan& p, long long M, int N, long long K, const void* a, long long stride_a, const void* b, long long stride_b,
-                              const LinearEpilogue& epi, float* out, float* parts, int sm_count, cudaStream_t stream);
+                              const LinearEpilogue& epi, float* out, float* parts, float* a_parts, int sm_count, cudaStream_t stream);
 // the forward product for up to kFewRows rows (linear_few.cu): rows of any length, no workspace
 constexpr int kFewRows = 8;
 cudaError_t launch_linear_few(bool e4m3, int rows, int n_in, int n_out, const void* x, const void* w, const LinearEpilogue& epi, cudaStream_t stream);

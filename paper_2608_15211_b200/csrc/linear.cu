@@ -14,7 +14,8 @@
 // The tensor cores' sum over k is not rounded to nearest, and its error grows with the number of steps.  The weight gradient, a sum over all
 // rows that comes out in fp32, therefore leaves TMEM every kChunk stages and is added up in registers.
 //
-// Roles (640 threads): warp 0 copies, warp 1 issues the products, warp 2 has the TMEM, warps 4-19 the epilogue.
+// Roles (640 threads): warp 0 copies, warp 1 issues the products, warp 2 has the TMEM, warps 4-19 the epilogue; weight gradient: warps 2 and 3 the
+// sums of d_z.
 // Every mbarrier wait is bounded; on expiry the CTA raises an abort flag, all roles leave their loops, TMEM is released and the host reads
 // the device status word.
 #include <cuda.h>
@@ -51,7 +52,7 @@ constexpr int kTile = 32 * 128;                        // a warp's 32 rows x 64 
 constexpr int kOffTiles = kStages * 2 * kOperand;
 constexpr int kOffBars = kOffTiles + kEpiWarpsMost * kTile;
 constexpr int kBFull = 0, kBEmpty = kStages, kBAccFull = 2 * kStages, kBAccEmpty = kBAccFull + 2, kBIn = kBAccEmpty + 2,
-              kBCount = kBIn + kEpiWarpsMost;
+              kBUsed = kBIn + kEpiWarpsMost, kBCount = kBUsed + kStages;
 constexpr int kOffTmem = kOffBars + 8 * kBCount, kOffAbort = kOffTmem + 4;
 constexpr int kSmem = kOffAbort + 4 + 1024;            // the base is rounded up to 1 KB
 constexpr int kAccCols = 256;                          // TMEM columns between the two accumulators
@@ -318,7 +319,8 @@ __global__ void __launch_bounds__(Roles<KIND>::kThreads, 1) linear_kernel(const 
     if (tid == 0) {
         for (int s = 0; s < kStages; ++s) {
             mbar_init(bar(kBFull + s), 1);
-            mbar_init(bar(kBEmpty + s), 1);
+            mbar_init(bar(kBEmpty + s), KIND == kLinearWeights ? 2 : 1);
+            mbar_init(bar(kBUsed + s), 1);
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(bar(kBAccFull + b), 1);
@@ -413,7 +415,7 @@ __global__ void __launch_bounds__(Roles<KIND>::kThreads, 1) linear_kernel(const 
                             mma<PAIR, E4M3>(acc, a, b, hi, job.idesc, accumulate);
 #pragma unroll
                             for (int k = 1; k < 4; ++k) mma<PAIR, E4M3>(acc, a + k * kALo, b + k * kBLo, hi, job.idesc, 1);
-                            commit<PAIR>(bar(kBEmpty + s));
+                            commit<PAIR>(bar((KIND == kLinearWeights ? kBUsed : kBEmpty) + s));
                         }
                         __syncwarp();
                         accumulate = 1;
@@ -427,7 +429,54 @@ __global__ void __launch_bounds__(Roles<KIND>::kThreads, 1) linear_kernel(const 
             }
         }
         __syncwarp();
-    } else if (warp >= kEpiWarp0) {
+    } else if (warp < kEpiWarp0) {
+        if constexpr (KIND == kLinearWeights) {
+            // Warps 2 and 3 hand the stages that the products have used back to the copies; on the way they add up the rows of A, 64 columns of d_z
+            // each: the bias's gradient.  The tiles of a row share the stages, every n_tiles-th to each.  (A pass over d_z of its own took 67 us of 935 at
+            // 156672 x 1024; all stages by the row's first tile made those tiles, and the kernel, 18 % slower.)
+            uint32_t s = 0, phase = 0;
+            bool ok = true;
+            for (; at.there() && ok; at.next()) {
+                float all[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+                const int k1 = at.k1();
+                uint32_t round, turn;                  // of this row's tiles, whose stage it is
+                job.by_n_tiles.split((uint32_t)at.k0(), round, turn);
+                for (int kb = at.k0(); kb < k1; ++kb) {
+                    ok = mbar_wait_all(bar(kBUsed + s), phase, cta_abort);
+                    if (!ok) break;
+                    if (job.e.a_sums && (int)turn == at.at.n) {
+                        const uint32_t box = base + s * 2 * kOperand + (warp - 2) * (kOperand / 2);
+                        float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+                        for (int i = 0; i < 16; ++i) {
+                            const int row = 4 * i + (lane >> 3);
+                            uint32_t v[4];
+                            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];\n" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
+                                         : "r"(box + place(row, lane & 7, false)) : "memory");
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) add_elems(sum[2 * q], sum[2 * q + 1], v[q]);
+                        }
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) all[c] += sum[c];
+                    }
+                    if ((int)++turn == job.n_tiles) turn = 0;
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(kBEmpty + s));
+                    if (++s == kStages) { s = 0; phase ^= 1; }
+                }
+                if (!ok || !job.e.a_sums) continue;
+                const long long m = at.m0(kTileRows) + 128 * rank + 64 * (warp - 2) + 8 * (lane & 7);
+                float* out = job.e.a_sums + ((size_t)at.at.split * job.n_tiles + at.at.n) * job.M;
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    all[c] += __shfl_xor_sync(0xffffffffu, all[c], 8);
+                    all[c] += __shfl_xor_sync(0xffffffffu, all[c], 16);
+                    if (lane < 8 && m + c < job.M) out[m + c] = all[c];
+                }
+            }
+        }
+        __syncwarp();
+    } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(R::kRegsEpi));
         // A chunk is 64 columns of the warp's 32 rows.  The chunks of all tiles go to the groups of four warps in turn: a warp has one or two of a tile,
         // or none of a narrow one.  (Every warp waits for every accumulator and gives it back, so that none falls behind by a phase.)
@@ -637,12 +686,20 @@ __global__ void __launch_bounds__(Roles<KIND>::kThreads, 1) linear_kernel(const 
 
 // Joins the parts of a split product: the sum over the splits, then the epilogue.
 template <int KIND>
-__global__ void __launch_bounds__(256) linear_join_kernel(const LinearEpilogue e, const float* __restrict__ parts, int splits, long long M, int N, float* out) {
+__global__ void __launch_bounds__(256) linear_join_kernel(const LinearEpilogue e, const float* __restrict__ parts, int splits, long long M, int N, float* out,
+                                                          const float* __restrict__ a_parts, int a_splits) {
     let_dependents_start();
     wait_for_prerequisites();
     const int per_row = (N + 3) / 4;
     const long long total = M * per_row;
     const bool wide = (N & 3) == 0;
+    if (KIND == kLinearWeights && a_parts)
+        for (long long i = blockIdx.x * 256ll + threadIdx.x; i < M; i += gridDim.x * 256ll) {
+            float v = 0.f;
+#pragma unroll 8
+            for (int s = 0; s < a_splits; ++s) v += a_parts[s * M + i];
+            e.a_sums[i] = v;
+        }
     for (long long i = blockIdx.x * 256ll + threadIdx.x; i < total; i += gridDim.x * 256ll) {
         long long row;
         int c4;
@@ -770,7 +827,7 @@ cudaError_t read_linear_status(int* timed_out) {
 
 // D[M, N] over K: operands given with their rows' strides in bytes (multiples of 16).  K-major operands are [M or N][K], MN-major ones [K][M or N].
 cudaError_t launch_linear(int kind, bool e4m3, const LinearPlan& p, long long M, int N, long long K, const void* a, long long stride_a, const void* b, long long stride_b,
-                          const LinearEpilogue& epi, float* out, float* parts, int sm_count, cudaStream_t stream) {
+                          const LinearEpilogue& epi, float* out, float* parts, float* a_parts, int sm_count, cudaStream_t stream) {
     const int ctas = p.pair ? 2 : 1, cols = p.bn / ctas, elem = e4m3 ? 1 : 2;
     const bool a_mn = kind == kLinearWeights, b_mn = kind != kLinearForward;
     Maps maps;
@@ -805,18 +862,21 @@ cudaError_t launch_linear(int kind, bool e4m3, const LinearPlan& p, long long M,
                      : make_idesc_elem(128 * ctas, p.bn, a_mn ? 1 : 0, b_mn ? 1 : 0);
     job.by_map = by_map;
     job.e = epi;
+    const int a_splits = epi.a_sums ? p.splits * p.n_tiles : 0;
+    if (a_splits > 1) job.e.a_sums = a_parts;
     job.e.sums = p.splits > 1 ? parts : kind == kLinearWeights ? out : nullptr;
     cudaError_t e;
     if (kind == kLinearForward && e4m3) e = p.pair ? launch_one<true, kLinearForward, true>(maps, job, sm_count, stream) : launch_one<false, kLinearForward, true>(maps, job, sm_count, stream);
     else if (kind == kLinearForward) e = p.pair ? launch_one<true, kLinearForward, false>(maps, job, sm_count, stream) : launch_one<false, kLinearForward, false>(maps, job, sm_count, stream);
     else if (kind == kLinearInput) e = p.pair ? launch_one<true, kLinearInput, false>(maps, job, sm_count, stream) : launch_one<false, kLinearInput, false>(maps, job, sm_count, stream);
     else e = p.pair ? launch_one<true, kLinearWeights, false>(maps, job, sm_count, stream) : launch_one<false, kLinearWeights, false>(maps, job, sm_count, stream);
+    if (e == cudaSuccess && p.splits == 1 && a_splits > 1) return launch_sum_partials(a_parts, a_splits, (int)M, epi.a_sums, stream);
     if (e != cudaSuccess || p.splits == 1) return e;
     const long long quads = M * ((N + 3) / 4), need = (quads + 255) / 256, fit = 8ll * sm_count;
     const unsigned grid = (unsigned)(need < fit ? need : fit);
     prof_begin("linear_join_kernel", stream);
     auto join = kind == kLinearForward ? linear_join_kernel<kLinearForward> : kind == kLinearInput ? linear_join_kernel<kLinearInput> : linear_join_kernel<kLinearWeights>;
-    e = launch_dependent(join, grid, 256u, 0, stream, epi, (const float*)parts, p.splits, M, N, out);
+    e = launch_dependent(join, grid, 256u, 0, stream, epi, (const float*)parts, p.splits, M, N, out, a_splits ? (const float*)a_parts : nullptr, a_splits);
     count_launch(stream);
     return e;
 }
