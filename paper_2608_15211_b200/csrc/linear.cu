@@ -109,6 +109,11 @@ __device__ __forceinline__ void arrive_leader(uint32_t bar) {
         mbar_arrive(bar);
 }
 
+// For roles that wait most of the time: they sleep between polls, which take issue slots from the epilogue's warps.
+__device__ __forceinline__ bool wait_asleep(uint32_t bar, uint32_t parity, volatile int* cta_abort) {
+    return __all_sync(0xffffffffu, mbar_wait<64>(bar, parity, cta_abort));
+}
+
 struct Maps { CUtensorMap a, b, in, y, z; };       // in: the residual or z_in
 __device__ __forceinline__ void store_box(const void* map, int x, int y, uint32_t src) {
     asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];\n" ::"l"(map), "r"(x), "r"(y), "r"(src) : "memory");
@@ -360,7 +365,7 @@ __global__ void __launch_bounds__(Roles<KIND>::kThreads, 1) linear_kernel(const 
         for (; at.there() && ok; at.next()) {
             const int m = (int)at.m0(kTileRows) + 128 * (int)rank, n = at.n0() + cols * (int)rank, k1 = at.k1();
             for (int kb = at.k0(); kb < k1; ++kb, ++it) {
-                ok = mbar_wait_all(bar(kBEmpty + s), phase, cta_abort);
+                ok = wait_asleep(bar(kBEmpty + s), phase, cta_abort);
                 if (!ok) break;
                 const uint32_t full = PAIR ? leaders(bar(kBFull + s)) : bar(kBFull + s), a = base + s * 2 * kOperand, b = a + kOperand;
                 if (elect_one()) {
@@ -402,7 +407,7 @@ __global__ void __launch_bounds__(Roles<KIND>::kThreads, 1) linear_kernel(const 
                 for (int kb = at.k0(); kb < k1 && ok;) {
                     const int end = KIND == kLinearWeights ? min(k1, kb + kLinearChunk) : k1;
                     const uint32_t buf = done & 1, acc = tmem + buf * kAccCols;
-                    ok = mbar_wait_all(bar(kBAccEmpty + buf), ((done >> 1) & 1) ^ 1u, cta_abort);
+                    ok = wait_asleep(bar(kBAccEmpty + buf), ((done >> 1) & 1) ^ 1u, cta_abort);
                     if (!ok) break;
                     tc_fence_after();
                     uint32_t accumulate = 0;
@@ -506,7 +511,7 @@ __global__ void __launch_bounds__(Roles<KIND>::kThreads, 1) linear_kernel(const 
                 for (int i = 0; i < 64; ++i) acc[i] = 0.f;
                 for (int kb = at.k0(); kb < k1 && ok; kb += kLinearChunk, ++done) {
                     const uint32_t buf = done & 1;
-                    ok = mbar_wait_all(bar(kBAccFull + buf), (done >> 1) & 1, cta_abort);
+                    ok = wait_asleep(bar(kBAccFull + buf), (done >> 1) & 1, cta_abort);
                     if (!ok) break;
                     tc_fence_after();
                     if (chunk < chunks)
@@ -538,7 +543,7 @@ __global__ void __launch_bounds__(Roles<KIND>::kThreads, 1) linear_kernel(const 
                 const long long row0 = at.m0(kTileRows) + 128 * rank + 32 * quarter;
                 const int n0 = at.n0();
                 const uint32_t buf = done & 1;
-                ok = mbar_wait_all(bar(kBAccFull + buf), (done >> 1) & 1, cta_abort);
+                ok = wait_asleep(bar(kBAccFull + buf), (done >> 1) & 1, cta_abort);
                 if (!ok) break;
                 tc_fence_after();
                 for (int chunk = first_chunk; chunk < chunks; chunk += kGroups) {
@@ -595,7 +600,7 @@ __global__ void __launch_bounds__(Roles<KIND>::kThreads, 1) linear_kernel(const 
                         if (E4M3) prefetch_l1(job.e.w_scale + c + 32 * lane);
                     }
                 }
-                ok = mbar_wait_all(bar(kBAccFull + buf), (done >> 1) & 1, cta_abort);
+                ok = wait_asleep(bar(kBAccFull + buf), (done >> 1) & 1, cta_abort);
                 if (!ok) {
                     if (mine && fetched && lane == 0) {       // it lands before this CTA ends
                         volatile int ignore = 0;
