@@ -2,9 +2,9 @@
 // y = h rstd weight, and its backward.  y in the activations' type or in e4m3 with one scale per token, scale = max|y| / 448.
 // h is stored rounded to the activations' type; y and rstd are taken of the unrounded sum, which is in registers.
 //
-// A token's row is held by `lanes` threads (a power of two, 4 to 1024), V vectors of E elements each, so that one read of the row
-// serves the sum of squares, the maximum and the output.  E = 8 (16-byte accesses) where the channels are a multiple of 8, else
-// single elements.  Blocks walk over the rows; the weights stay in registers.  All sums in fp32.
+// A token's row is held by `lanes` threads (a power of two, 4 to 512), V vectors of E elements each, so that one read of the row
+// serves the sum of squares, the maximum and the output.  E is 8, 2 or 1 as the channels allow.  Blocks walk over the rows, the next row's reads
+// under way while a row is worked on; the weights stay in registers.  All sums in fp32.
 #include <cuda_fp8.h>
 
 #include "block_kernels.h"
@@ -18,6 +18,7 @@ namespace terra {
 namespace {
 
 constexpr int kBlock = 256;            // threads of a block where a row takes no more
+constexpr int kMaxLanes = 512;         // threads of a row at most
 constexpr float kE4m3Max = 448.f;
 
 // E elements of a row as they lie in memory
@@ -32,6 +33,12 @@ template <> struct Raw<8> {
         for (int i = 0; i < 4; ++i) { const float2 t = elem2_to_float2(w[i]); f[2 * i] = t.x; f[2 * i + 1] = t.y; }
     }
 };
+template <> struct Raw<2> {
+    uint32_t v;
+    __device__ void load(const uint16_t* p) { v = *reinterpret_cast<const uint32_t*>(p); }
+    __device__ void zero() { v = 0; }
+    __device__ void floats(float (&f)[2]) const { const float2 t = elem2_to_float2(v); f[0] = t.x; f[1] = t.y; }
+};
 template <> struct Raw<1> {
     uint32_t v;
     __device__ void load(const uint16_t* p) { v = *p; }
@@ -41,11 +48,13 @@ template <> struct Raw<1> {
 __device__ __forceinline__ void store(uint16_t* p, const float (&f)[8]) {
     *reinterpret_cast<uint4*>(p) = make_uint4(pack_elem(f[0], f[1]), pack_elem(f[2], f[3]), pack_elem(f[4], f[5]), pack_elem(f[6], f[7]));
 }
+__device__ __forceinline__ void store(uint16_t* p, const float (&f)[2]) { *reinterpret_cast<uint32_t*>(p) = pack_elem(f[0], f[1]); }
 __device__ __forceinline__ void store(uint16_t* p, const float (&f)[1]) { *p = (uint16_t)pack_elem(f[0], 0.f); }
 __device__ __forceinline__ uint32_t pack_e4m3(float a, float b) { return __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3); }
 __device__ __forceinline__ void store_e4m3(uint8_t* p, const float (&f)[8]) {
     *reinterpret_cast<uint2*>(p) = make_uint2(pack_e4m3(f[0], f[1]) | pack_e4m3(f[2], f[3]) << 16, pack_e4m3(f[4], f[5]) | pack_e4m3(f[6], f[7]) << 16);
 }
+__device__ __forceinline__ void store_e4m3(uint8_t* p, const float (&f)[2]) { *reinterpret_cast<uint16_t*>(p) = (uint16_t)pack_e4m3(f[0], f[1]); }
 __device__ __forceinline__ void store_e4m3(uint8_t* p, const float (&f)[1]) { *p = (uint8_t)pack_e4m3(f[0], 0.f); }
 
 __device__ __forceinline__ float max_nan(float a, float b) {       // a NaN stays one
@@ -74,9 +83,9 @@ __device__ __forceinline__ float over_row(float s, int lanes, float* buf, int& t
     return s;
 }
 
-// What bounds it: HBM.
+// What bounds it: HBM (156672 x 4096 785 us, 6.5 TB/s; e4m3 861 us, 5.2 TB/s).
 template <int E, int V, bool E4M3>
-__global__ void __launch_bounds__(E == 8 ? 512 : 1024)
+__global__ void __launch_bounds__(kMaxLanes, E == 8 && V <= 2 ? 2 : 1)
 rms_norm_fwd_kernel(const NormArgs a, int lanes, int lanes_log2) {
     __shared__ float buf[64];
     int turn = 0;
@@ -93,21 +102,29 @@ rms_norm_fwd_kernel(const NormArgs a, int lanes, int lanes_log2) {
         }
     const uint16_t *x = (const uint16_t*)a.x, *r = (const uint16_t*)a.r;
     uint16_t* h = (uint16_t*)a.h;
-    for (long long row0 = (long long)blockIdx.x * per_block; row0 < a.rows; row0 += (long long)gridDim.x * per_block) {
-        const long long row = row0 + sub;
-        const bool live = row < a.rows;
-        const long long at = row * a.channels;
-        Raw<E> xr[V], rr[V];
+    Raw<E> xr[V], rr[V];
+    auto fetch = [&](long long row) {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int c = lane + v * lanes;
             xr[v].zero();
             rr[v].zero();
-            if (live && c < chunks) {
-                xr[v].load(x + at + c * E);
-                if (r) rr[v].load(r + at + c * E);
+            if (row < a.rows && c < chunks) {
+                xr[v].load(x + row * a.channels + c * E);
+                if (r) rr[v].load(r + row * a.channels + c * E);
             }
         }
+    };
+    const long long step = (long long)gridDim.x * per_block;
+    // (With the residual's reads and the sum's writes beside a 16-bit output, reads ahead make it slower: 156672 x 4096 789 -> 878 us.  Without the residual
+    // they take it from 535 to 481 us, with the output in 8 bits from 938 to 861.)
+    const bool ahead = E4M3 || !r;
+    if (ahead) fetch((long long)blockIdx.x * per_block + sub);
+    for (long long row0 = (long long)blockIdx.x * per_block; row0 < a.rows; row0 += step) {
+        const long long row = row0 + sub;
+        const bool live = row < a.rows;
+        const long long at = row * a.channels;
+        if (!ahead) fetch(row);
         float f[V][E], sum = 0.f;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
@@ -118,6 +135,10 @@ rms_norm_fwd_kernel(const NormArgs a, int lanes, int lanes_log2) {
 #pragma unroll
                 for (int e = 0; e < E; ++e) f[v][e] += t[e];
             }
+        }
+        if (ahead) fetch(row + step);  // (rows of other blocks are not written, so outputs over inputs stay right)
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
 #pragma unroll
             for (int e = 0; e < E; ++e) sum = fmaf(f[v][e], f[v][e], sum);
             const int c = lane + v * lanes;
@@ -161,9 +182,9 @@ rms_norm_fwd_kernel(const NormArgs a, int lanes, int lanes_log2) {
 
 // n = h rstd, g = d_y weight: dx = rstd (g - n mean(g n)) + d_h, dweight = sum over the rows of d_y n.  A block adds up its rows'
 // dweight in registers and writes one row of `partial`; sum_partials_kernel adds those in a fixed order.
-// What bounds it: HBM.
+// What bounds it: HBM (156672 x 4096 807 us, 131072 x 768 135 us, 6.0 to 6.4 TB/s).
 template <int E, int V>
-__global__ void __launch_bounds__(E == 8 ? 512 : 1024)
+__global__ void __launch_bounds__(kMaxLanes)
 rms_norm_bwd_kernel(const NormArgs a, int lanes, int lanes_log2) {
     __shared__ float buf[64];
     extern __shared__ float groups_sum[];
@@ -182,46 +203,57 @@ rms_norm_bwd_kernel(const NormArgs a, int lanes, int lanes_log2) {
             acc[v][e] = 0.f;
         }
     const uint16_t *h = (const uint16_t*)a.x, *dh = (const uint16_t*)a.r, *dy = (const uint16_t*)a.d_y;
-    for (long long row0 = (long long)blockIdx.x * per_block; row0 < a.rows; row0 += (long long)gridDim.x * per_block) {
-        const long long row = row0 + sub;
-        const bool live = row < a.rows;
-        const long long at = row * a.channels;
-        Raw<E> hr[V], gr[V], dr[V];
+    constexpr bool kAhead = V * E <= 16;       // the next row's reads are under way while this one is worked on (else the registers do not hold both)
+    Raw<E> hr[V], gr[V], dr[V];
+    float rstd = 0.f;
+    auto fetch = [&](long long row) {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int c = lane + v * lanes;
             hr[v].zero();
             gr[v].zero();
             dr[v].zero();
-            if (live && c < chunks) {
-                hr[v].load(h + at + c * E);
-                gr[v].load(dy + at + c * E);
-                if (dh) dr[v].load(dh + at + c * E);
+            if (row < a.rows && c < chunks) {
+                hr[v].load(h + row * a.channels + c * E);
+                gr[v].load(dy + row * a.channels + c * E);
+                if (dh) dr[v].load(dh + row * a.channels + c * E);
             }
         }
-        const float rstd = live ? a.rstd_in[row] : 0.f;
-        float along = 0.f;
+        rstd = row < a.rows ? a.rstd_in[row] : 0.f;
+    };
+    const long long step = (long long)gridDim.x * per_block;
+    if (kAhead) fetch((long long)blockIdx.x * per_block + sub);
+    for (long long row0 = (long long)blockIdx.x * per_block; row0 < a.rows; row0 += step) {
+        const long long row = row0 + sub;
+        const bool live = row < a.rows;
+        const long long at = row * a.channels;
+        if (!kAhead) fetch(row);
+        float n[V][E], g[V][E], along = 0.f;
+        Raw<E> dn[V];
+        const float rs = rstd;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            float n[E], g[E];
-            hr[v].floats(n);
-            gr[v].floats(g);
+            hr[v].floats(n[v]);
+            gr[v].floats(g[v]);
+            dn[v] = dr[v];
+        }
+        if (kAhead) fetch(row + step);
+#pragma unroll
+        for (int v = 0; v < V; ++v)
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                const float t = n[e] * rstd * g[e];
+                n[v][e] *= rs;
+                const float t = n[v][e] * g[v][e];
                 acc[v][e] += t;
                 along = fmaf(t, w[v][e], along);
             }
-        }
         along = over_row<false>(along, lanes, buf, turn) * per_channel;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            float n[E], g[E], d[E];
-            hr[v].floats(n);
-            gr[v].floats(g);
-            dr[v].floats(d);
+            float d[E];
+            dn[v].floats(d);
 #pragma unroll
-            for (int e = 0; e < E; ++e) d[e] = fmaf(rstd, fmaf(g[e], w[v][e], -n[e] * rstd * along), d[e]);
+            for (int e = 0; e < E; ++e) d[e] = fmaf(rs, fmaf(g[v][e], w[v][e], -n[v][e] * along), d[e]);
             const int c = lane + v * lanes;
             if (live && c < chunks) store((uint16_t*)a.y + at + c * E, d);
         }
@@ -254,24 +286,31 @@ rms_norm_bwd_kernel(const NormArgs a, int lanes, int lanes_log2) {
 
 struct Shape { int E, V, lanes, lanes_log2, threads; };
 
-// Threads to a row: with 16-byte vectors the fewest (but 4 at least) of up to 4 vectors each.  V is the number that
-// the row needs then, so that 96, 192, 384 and 768 channels (3 vectors) leave no thread idle.
-Shape shape_for(int channels) {
+// Threads to a row: the fewest (but 4 at least) of up to `most` vectors each.  With 16-byte vectors V is the number that the row needs
+// then, so that 96, 192, 384 and 768 channels (3 vectors) leave no thread idle.  Up to 4 vectors in a warp; in rows of several warps 2, which leaves
+// registers for the next row's (156672 x 4096, with the next row ahead: forward 806 -> 785 us, e4m3 976 -> 861, backward 1661 -> 807).  Odd and even
+// numbers of channels by 2 and 4 bytes a thread: 300000 x 1001 forward 773 us, x 1002 549, x 1000 396.
+Shape shape_for(int channels, bool backward) {
     Shape s;
-    s.E = channels % 8 == 0 ? 8 : 1;
-    const int chunks = channels / s.E, most = s.E == 8 ? 4 : chunks <= 4096 ? 4 : 16;
+    s.E = channels % 8 == 0 ? 8 : channels % 2 == 0 ? 2 : 1;
+    const int chunks = channels / s.E;
+    int most;
+    if (s.E == 8) most = chunks > (backward ? 96 : 128) && chunks <= 1024 ? 2 : 4;
+    else if (s.E == 2) most = chunks <= 8 * kMaxLanes ? 8 : 16;
+    else if (backward) most = chunks <= 4 * kMaxLanes ? 4 : chunks <= 8 * kMaxLanes ? 8 : chunks <= 16 * kMaxLanes ? 16 : 32;
+    else most = chunks <= 64 ? 4 : chunks <= 16 * kMaxLanes ? 16 : 32;
     s.lanes = 4;
     s.lanes_log2 = 2;
     while (s.lanes * most < chunks) { s.lanes *= 2; ++s.lanes_log2; }
-    s.V = (chunks + s.lanes - 1) / s.lanes;
-    if (s.E == 1) s.V = most;
+    s.V = s.E == 8 ? (chunks + s.lanes - 1) / s.lanes : most;
     s.threads = s.lanes < kBlock ? kBlock : s.lanes;
     return s;
 }
 
 template <bool E4M3>
 auto fwd_kernel(const Shape& s) {
-    if (s.E == 1) return s.V == 4 ? rms_norm_fwd_kernel<1, 4, E4M3> : rms_norm_fwd_kernel<1, 16, E4M3>;
+    if (s.E == 1) return s.V == 4 ? rms_norm_fwd_kernel<1, 4, E4M3> : s.V == 16 ? rms_norm_fwd_kernel<1, 16, E4M3> : rms_norm_fwd_kernel<1, 32, E4M3>;
+    if (s.E == 2) return s.V == 8 ? rms_norm_fwd_kernel<2, 8, E4M3> : rms_norm_fwd_kernel<2, 16, E4M3>;
     switch (s.V) {
         case 1: return rms_norm_fwd_kernel<8, 1, E4M3>;
         case 2: return rms_norm_fwd_kernel<8, 2, E4M3>;
@@ -280,7 +319,8 @@ auto fwd_kernel(const Shape& s) {
     }
 }
 auto bwd_kernel(const Shape& s) {
-    if (s.E == 1) return s.V == 4 ? rms_norm_bwd_kernel<1, 4> : rms_norm_bwd_kernel<1, 16>;
+    if (s.E == 1) return s.V == 4 ? rms_norm_bwd_kernel<1, 4> : s.V == 8 ? rms_norm_bwd_kernel<1, 8> : s.V == 16 ? rms_norm_bwd_kernel<1, 16> : rms_norm_bwd_kernel<1, 32>;
+    if (s.E == 2) return s.V == 8 ? rms_norm_bwd_kernel<2, 8> : rms_norm_bwd_kernel<2, 16>;
     switch (s.V) {
         case 1: return rms_norm_bwd_kernel<8, 1>;
         case 2: return rms_norm_bwd_kernel<8, 2>;
@@ -295,14 +335,14 @@ constexpr int kBwdBlocks = 640;        // rows of `partial` at most
 
 #ifndef TERRA_ELEM_F16
 int norm_bwd_blocks(long long rows, int channels) {
-    const Shape s = shape_for(channels);
+    const Shape s = shape_for(channels, true);
     const long long per_block = s.threads / s.lanes, need = (rows + per_block - 1) / per_block;
     return (int)(need < kBwdBlocks ? need : kBwdBlocks);
 }
 #endif
 
 cudaError_t launch_rms_norm_fwd(const NormArgs& a, int sm_count, cudaStream_t stream) {
-    const Shape s = shape_for(a.channels);
+    const Shape s = shape_for(a.channels, false);
     auto kern = a.scale ? fwd_kernel<true>(s) : fwd_kernel<false>(s);
     int occ = 1;
     cudaError_t e = prepare_kernel((const void*)kern, 0, s.threads, &occ);
@@ -315,7 +355,7 @@ cudaError_t launch_rms_norm_fwd(const NormArgs& a, int sm_count, cudaStream_t st
 }
 
 cudaError_t launch_rms_norm_bwd(const NormArgs& a, int sm_count, cudaStream_t stream) {
-    const Shape s = shape_for(a.channels);
+    const Shape s = shape_for(a.channels, true);
     auto kern = bwd_kernel(s);
     const int wide = s.lanes < 32 ? 32 : s.lanes, groups = s.threads / wide;
     const size_t smem = groups > 1 ? (size_t)groups * a.channels * sizeof(float) : 0;

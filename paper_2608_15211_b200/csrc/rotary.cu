@@ -4,7 +4,7 @@
 // frame that the windows tile ((u - shift) mod H: the tokens of a window that lies over the seam have consecutive positions), or by given positions.
 //
 // A block takes a few tokens: first the angles of all their pairs (in fp64: position 10^7 times a frequency leaves fp32 no digit behind
-// the point; reduced to +-pi, then cos and sin in fp32) into shared memory, once for all heads of q and k, then the heads by 16-byte
+// the point; reduced to half a turn, then cos and sin in fp32) into shared memory, once for all heads of q and k, then the heads by 16-byte
 // accesses.  A thread reads all that it writes before it writes, so the outputs may be the inputs.
 // What bounds it: HBM.
 #include "block_kernels.h"
@@ -66,11 +66,9 @@ __global__ void __launch_bounds__(kBlock) rotary_kernel(const RotaryArgs a, cons
             if ((int)p < a.row_pairs) pos = u >= a.sh ? u - a.sh : u - a.sh + a.H;
             else pos = v >= a.sw ? v - a.sw : v - a.sw + a.W;
         }
-        const double angle = (double)pos * a.freq[p];
-        const double whole = rint(angle * 0.15915494309189535);                                    // 1 / (2 pi)
-        const double rest = fma(-whole, 2.4492935982947064e-16, fma(-whole, 6.283185307179586, angle));   // 2 pi in two parts
+        const double turns = (double)pos * a.freq[p] * 0.15915494309189535;       // 1 / (2 pi)
         float s, c;
-        sincosf((float)rest, &s, &c);
+        sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
         turn[i] = make_float2(c * a.scale, (a.inverse ? -s : s) * a.scale);
     }
     __syncthreads();

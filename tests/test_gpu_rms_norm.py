@@ -11,7 +11,7 @@ BF16, F16 = torch.bfloat16, torch.float16
 REL = 2.0 ** -18
 
 # rows, channels: one thread's vector, rows of 2 to 512 threads, odd channels (single elements), one row and odd numbers of rows
-SHAPES = [(1, 8), (7, 1), (33, 96), (5, 13), (64, 128), (2048, 96), (129, 384), (70, 768), (9, 1024), (3, 1040), (5, 1001), (11, 4096), (2, 4097), (3, 8192), (2, 16384), (1, 16383)]
+SHAPES = [(1, 8), (7, 1), (33, 96), (5, 13), (64, 128), (2048, 96), (129, 384), (70, 768), (9, 1024), (3, 1040), (5, 1001), (11, 4096), (2, 4097), (3, 8192), (2, 16384), (1, 16383), (37, 372), (6, 1860), (9, 2002), (4, 5000), (3, 8190), (2, 16380)]
 
 
 def draw(rows, channels, dtype, seed=0):
