@@ -34,7 +34,7 @@ def wanted(cfg, x, freq, row_pairs, layout, scale, inverse, positions=None):
 CASES = [  # B, H, W, heads, d, shift_h, shift_w, rot, row_pairs, dtype
     (1, 1, 1, 1, 32, 0, 0, 32, 0, BF16), (2, 5, 7, 3, 32, 2, 3, 32, 8, BF16), (1, 13, 9, 2, 64, 4, 4, 32, 8, F16), (1, 3, 70, 5, 128, 0, 8, 128, 32, BF16),
     (1, 6, 11, 2, 32, 1, 2, 20, 5, BF16), (1, 6, 11, 2, 64, 1, 2, 22, 11, F16), (1, 4, 5, 1, 128, 0, 0, 126, 1, BF16), (1, 9, 9, 2, 32, 0, 0, 2, 1, BF16),
-    (1, 2, 3, 131, 32, 1, 1, 32, 8, BF16), (3, 40, 30, 6, 32, 4, 4, 16, 4, F16), (1, 1, 700, 4, 64, 0, 0, 48, 0, BF16),
+    (1, 2, 3, 131, 32, 1, 1, 32, 8, BF16), (1, 3, 5, 3, 128, 1, 1, 110, 20, BF16), (1, 3, 5, 2, 64, 0, 1, 36, 18, F16), (2, 3, 4, 2, 32, 1, 0, 6, 1, BF16), (3, 40, 30, 6, 32, 4, 4, 16, 4, F16), (1, 1, 700, 4, 64, 0, 0, 48, 0, BF16),
 ]
 
 
