@@ -182,7 +182,8 @@ static LinearPlan make_plan(int kind, bool e4m3, long long M, int N, long long K
         const long long m_tiles = (M + 128 * ctas - 1) / (128 * ctas);
         for (int bn = 32; bn <= 128 * ctas; bn += 32) {
             const int n_tiles = (N + bn - 1) / bn;
-            if (bn > 32 && (N + bn - 33) / (bn - 32) == n_tiles) continue;        // a narrower tile does with as many
+            if (bn % 64 && n_tiles > 1) continue;      // the epilogue's 64 columns would reach into the next tile
+            if (bn > 32 && n_tiles == (n_tiles > 1 ? (N + bn - 65) / (bn - 64 > 0 ? bn - 64 : 1) : (N + bn - 33) / (bn - 32))) continue;        // a narrower tile does with as many
             const double operand = 128. * 128 + 128. * bn / ctas;
             const double step = 2. * bn > operand / 48 ? 2. * bn : operand / 48;
             for (int want = 1; want <= 64; ++want) {

@@ -135,7 +135,6 @@ struct Job {
     int bytes_b;                               // of a CTA's share of B in a stage
     int boxes_b;                               // MN-major: boxes of 64 columns
     uint32_t idesc;
-    int by_map;                                // rows of the outputs are multiples of 16 bytes: the copy engine moves them
     LinearEpilogue e;
 };
 
@@ -214,29 +213,41 @@ __device__ __forceinline__ uint32_t place(int row, int at, bool narrow) {
     return narrow ? row * 64 + ((at ^ ((row >> 1) & 3)) << 4) : row * 128 + ((at ^ (row & 7)) << 4);
 }
 
+__device__ __forceinline__ void lds(uint32_t at, unsigned long long& v) { asm volatile("ld.shared.b64 %0, [%1];\n" : "=l"(v) : "r"(at) : "memory"); }
+__device__ __forceinline__ void lds(uint32_t at, uint32_t& v) { asm volatile("ld.shared.b32 %0, [%1];\n" : "=r"(v) : "r"(at) : "memory"); }
+__device__ __forceinline__ void lds(uint32_t at, uint16_t& v) { asm volatile("ld.shared.b16 %0, [%1];\n" : "=h"(v) : "r"(at) : "memory"); }
+__device__ __forceinline__ void sts(uint32_t at, unsigned long long v) { asm volatile("st.shared.b64 [%0], %1;\n" ::"r"(at), "l"(v) : "memory"); }
+__device__ __forceinline__ void sts(uint32_t at, uint32_t v) { asm volatile("st.shared.b32 [%0], %1;\n" ::"r"(at), "r"(v) : "memory"); }
+__device__ __forceinline__ void sts(uint32_t at, uint16_t v) { asm volatile("st.shared.b16 [%0], %1;\n" ::"r"(at), "h"(v) : "memory"); }
+
 // A warp's tile <-> `rows` rows of global memory from g on (its first row and column; rows of `stride` elements), the first `cols` columns, in units
-// of T: for rows that are no multiples of 16 bytes, and tiles that end inside 64 columns.
+// of T: for rows that are no multiples of 16 bytes.  Eight rows (of 8-byte units sixteen) are read before they are written.
 template <bool OUT, typename T>
-__device__ __forceinline__ void copy_tile_units(uint8_t* tile, bool narrow, uint16_t* g, long long stride, int rows, int cols, int lane) {
+__device__ __forceinline__ void copy_tile_units(uint32_t tile, bool narrow, uint16_t* g, long long stride, int rows, int cols, int lane) {
     constexpr int kUnit = sizeof(T) / 2, kAcross = 64 / kUnit, kLanes = kAcross < 32 ? kAcross : 32, kDown = 32 / kLanes;
-    const int sub = lane / kLanes, first = lane % kLanes;
+    const int sub = lane / kLanes;
+#pragma unroll 1
+    for (int col = (lane % kLanes) * kUnit; col < cols; col += kLanes * kUnit) {
+        uint16_t* p = g + sub * stride + col;
+        const uint32_t in_place = (col & 7) * 2;
+#pragma unroll 1
+        for (int r = sub; r < rows; r += 8 * kDown, p += 8 * kDown * stride) {
+            T v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
-    for (int part = 0; part < kAcross / kLanes; ++part) {
-        const int col = (first + part * kLanes) * kUnit;
-        if (col >= cols) continue;
-#pragma unroll 8
-        for (int r0 = 0; r0 < 32; r0 += kDown) {
-            const int r = r0 + sub;
-            T* at = reinterpret_cast<T*>(tile + place(r, col >> 3, narrow) + (col & 7) * 2);
-            if (r < rows) {
-                if (OUT) *reinterpret_cast<T*>(g + r * stride + col) = *at;
-                else *at = *reinterpret_cast<const T*>(g + r * stride + col);
+            for (int i = 0; i < 8; ++i) {
+                if (OUT) lds(tile + place(r + i * kDown, col >> 3, narrow) + in_place, v[i]);
+                else if (r + i * kDown < rows) v[i] = *reinterpret_cast<const T*>(p + i * kDown * stride);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (!OUT) sts(tile + place(r + i * kDown, col >> 3, narrow) + in_place, v[i]);
+                else if (r + i * kDown < rows) *reinterpret_cast<T*>(p + i * kDown * stride) = v[i];
             }
         }
     }
 }
 template <bool OUT>
-__device__ __noinline__ void copy_tile(uint8_t* tile, bool narrow, uint16_t* g, long long stride, int rows, int cols, int lane) {
+__device__ __forceinline__ void copy_tile(uint32_t tile, bool narrow, uint16_t* g, long long stride, int rows, int cols, int lane) {
     if (((stride | cols) & 3) == 0) copy_tile_units<OUT, unsigned long long>(tile, narrow, g, stride, rows, cols, lane);
     else if (((stride | cols) & 1) == 0) copy_tile_units<OUT, uint32_t>(tile, narrow, g, stride, rows, cols, lane);
     else copy_tile_units<OUT, uint16_t>(tile, narrow, g, stride, rows, cols, lane);
@@ -286,10 +297,10 @@ __device__ __forceinline__ void put_sums(uint32_t tile, int lane, int part, cons
         asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};\n" ::"r"(tile + place(lane, 4 * part + c, false)), "f"(v[4 * c]), "f"(v[4 * c + 1]), "f"(v[4 * c + 2]),
                      "f"(v[4 * c + 3]) : "memory");
 }
-__device__ __noinline__ void write_sums(uint32_t tile, float* out, long long M, int N, long long row0, int col0, int lane) {
+__device__ __forceinline__ void write_sums(uint32_t tile, float* out, long long M, int N, long long row0, int col0, int lane) {
     const int j = lane & 7, col = col0 + 4 * j;
     if (col >= N) return;
-#pragma unroll
+#pragma unroll 4
     for (int i = 0; i < 8; ++i) {
         const int r = 4 * i + (lane >> 3);
         float v[4];
@@ -306,7 +317,9 @@ __device__ __noinline__ void write_sums(uint32_t tile, float* out, long long M, 
     }
 }
 
-template <bool PAIR, int KIND, bool E4M3>
+// MAP: the rows of the outputs (and of the residual or z_in) are multiples of 16 bytes and the copy engine moves them; else the warps do.  (One kernel with
+// both spilled registers around the warps' copies: 2203200 x 256 -> 384 558 -> 1032 us.)
+template <bool PAIR, int KIND, bool E4M3, bool MAP>
 __global__ void __launch_bounds__(Roles<KIND>::kThreads, 1) linear_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Job job) {
     constexpr int CTAS = PAIR ? 2 : 1;
     using R = Roles<KIND>;
@@ -486,8 +499,7 @@ __global__ void __launch_bounds__(Roles<KIND>::kThreads, 1) linear_kernel(const 
         // A chunk is 64 columns of the warp's 32 rows.  The chunks of all tiles go to the groups of four warps in turn: a warp has one or two of a tile,
         // or none of a narrow one.  (Every warp waits for every accumulator and gives it back, so that none falls behind by a phase.)
         const int quarter = warp & 3, group = (warp - kEpiWarp0) >> 2, chunks = (job.bn + 63) >> 6;
-        uint8_t* tile_p = smem + kOffTiles + (warp - kEpiWarp0) * kTile;
-        const uint32_t tile = smem_u32(tile_p);
+        const uint32_t tile = base + kOffTiles + (warp - kEpiWarp0) * kTile;
         const uint32_t lane_tmem = tmem + ((uint32_t)(quarter * 32) << 16);
         uint32_t done = 0;
         bool ok = true;
@@ -581,7 +593,7 @@ __global__ void __launch_bounds__(Roles<KIND>::kThreads, 1) linear_kernel(const 
                 const uint32_t buf = done & 1, acc = lane_tmem + buf * kAccCols;
                 const int rows = (int)min(32ll, job.M - row0);
                 // (rows <= 0: the tile's last rows are no rows)
-                const bool fetched = has_in && job.by_map;
+                const bool fetched = MAP && has_in;
                 auto prepare = [&](int col) {          // by one lane
                     stores_read<0>();                  // the tile is free
                     if (fetched) {
@@ -614,7 +626,6 @@ __global__ void __launch_bounds__(Roles<KIND>::kThreads, 1) linear_kernel(const 
                     const int col0 = 64 * chunk, col = n0 + col0, cols = min(64, job.bn - col0), own = min(cols, job.N - col);
                     uint32_t cur[32];
                     tmem_ld32(acc + col0, cur);
-                    const bool engine = job.by_map && (has_z || cols == 64 || col + cols >= job.N);     // else the tile's last columns are a neighbour's
                     float x_scale = 1.f;
                     if (E4M3 && lane < rows) x_scale = __ldg(job.e.x_scale + row0 + lane);
 #pragma unroll 1
@@ -631,8 +642,8 @@ __global__ void __launch_bounds__(Roles<KIND>::kThreads, 1) linear_kernel(const 
                                     break;
                                 }
                                 ++n_in;
-                            } else if (has_in) {
-                                if (own > p0) copy_tile<false>(tile_p, has_z, (uint16_t*)in + row0 * job.N + col + p0, job.N, rows, min(width, own - p0), lane);
+                            } else if (!MAP && has_in) {
+                                if (own > p0) copy_tile<false>(tile, has_z, (uint16_t*)in + row0 * job.N + col + p0, job.N, rows, min(width, own - p0), lane);
                                 __syncwarp();
                             }
                         }
@@ -650,7 +661,7 @@ __global__ void __launch_bounds__(Roles<KIND>::kThreads, 1) linear_kernel(const 
                         });
                         if (!has_z && p0 + 32 < cols) continue;
                         const int at = has_z ? p0 : 0; // the tile's first column
-                        if (engine) {
+                        if (MAP) {
                             fence_proxy_async();
                             __syncwarp();
                             if (lane == 0) {
@@ -662,8 +673,8 @@ __global__ void __launch_bounds__(Roles<KIND>::kThreads, 1) linear_kernel(const 
                             __syncwarp();
                             if (own > at) {
                                 const long long where = row0 * job.N + col + at;
-                                copy_tile<true>(tile_p, has_z, (uint16_t*)job.e.y + where, job.N, rows, min(width, own - at), lane);
-                                if (has_z) copy_tile<true>(tile_p + kTile / 2, true, (uint16_t*)job.e.z + where, job.N, rows, min(width, own - at), lane);
+                                copy_tile<true>(tile, has_z, (uint16_t*)job.e.y + where, job.N, rows, min(width, own - at), lane);
+                                if (has_z) copy_tile<true>(tile + kTile / 2, true, (uint16_t*)job.e.z + where, job.N, rows, min(width, own - at), lane);
                             }
                             __syncwarp();
                         }
@@ -793,9 +804,9 @@ bool encode_map(CUtensorMap* map, const void* base, long long fast, long long sl
                CU_TENSOR_MAP_INTERLEAVE_NONE, box_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <bool PAIR, int KIND, bool E4M3>
+template <bool PAIR, int KIND, bool E4M3, bool MAP>
 cudaError_t launch_one(const Maps& maps, Job& job, int sm_count, cudaStream_t stream) {
-    auto kern = linear_kernel<PAIR, KIND, E4M3>;
+    auto kern = linear_kernel<PAIR, KIND, E4M3, MAP>;
     cudaError_t e = prepare_kernel((const void*)kern, kSmem);
     if (e != cudaSuccess) return e;
     const unsigned units = (unsigned)(job.groups * job.group * job.n_tiles * job.splits), fit = (unsigned)sm_count / (PAIR ? 2 : 1), at_a_time = units < fit ? units : fit;
@@ -818,6 +829,12 @@ cudaError_t launch_one(const Maps& maps, Job& job, int sm_count, cudaStream_t st
     e = cudaLaunchKernelEx(&cfg, kern, maps, job);
     count_launch(stream);
     return e;
+}
+
+template <int KIND, bool E4M3>
+cudaError_t launch_kind(bool pair, bool map, const Maps& maps, Job& job, int sm_count, cudaStream_t stream) {
+    if (pair) return map ? launch_one<true, KIND, E4M3, true>(maps, job, sm_count, stream) : launch_one<true, KIND, E4M3, false>(maps, job, sm_count, stream);
+    return map ? launch_one<false, KIND, E4M3, true>(maps, job, sm_count, stream) : launch_one<false, KIND, E4M3, false>(maps, job, sm_count, stream);
 }
 
 }  // namespace
@@ -865,16 +882,17 @@ cudaError_t launch_linear(int kind, bool e4m3, const LinearPlan& p, long long M,
     job.bytes_b = b_mn ? job.boxes_b * (kOperand / 2) : cols * 128;
     job.idesc = e4m3 ? make_idesc_f16(128 * ctas, p.bn, 0, 0)            // e4m3 has format number 0, as fp16 has in its kind
                      : make_idesc_elem(128 * ctas, p.bn, a_mn ? 1 : 0, b_mn ? 1 : 0);
-    job.by_map = by_map;
     job.e = epi;
     const int a_splits = epi.a_sums ? p.splits * p.n_tiles : 0;
     if (a_splits > 1) job.e.a_sums = a_parts;
     job.e.sums = p.splits > 1 ? parts : kind == kLinearWeights ? out : nullptr;
+    // (a part of a split sum goes neither way)
+    const bool map = by_map || p.splits > 1;
     cudaError_t e;
-    if (kind == kLinearForward && e4m3) e = p.pair ? launch_one<true, kLinearForward, true>(maps, job, sm_count, stream) : launch_one<false, kLinearForward, true>(maps, job, sm_count, stream);
-    else if (kind == kLinearForward) e = p.pair ? launch_one<true, kLinearForward, false>(maps, job, sm_count, stream) : launch_one<false, kLinearForward, false>(maps, job, sm_count, stream);
-    else if (kind == kLinearInput) e = p.pair ? launch_one<true, kLinearInput, false>(maps, job, sm_count, stream) : launch_one<false, kLinearInput, false>(maps, job, sm_count, stream);
-    else e = p.pair ? launch_one<true, kLinearWeights, false>(maps, job, sm_count, stream) : launch_one<false, kLinearWeights, false>(maps, job, sm_count, stream);
+    if (kind == kLinearForward && e4m3) e = launch_kind<kLinearForward, true>(p.pair, map, maps, job, sm_count, stream);
+    else if (kind == kLinearForward) e = launch_kind<kLinearForward, false>(p.pair, map, maps, job, sm_count, stream);
+    else if (kind == kLinearInput) e = launch_kind<kLinearInput, false>(p.pair, map, maps, job, sm_count, stream);
+    else e = p.pair ? launch_one<true, kLinearWeights, false, true>(maps, job, sm_count, stream) : launch_one<false, kLinearWeights, false, true>(maps, job, sm_count, stream);
     if (e == cudaSuccess && p.splits == 1 && a_splits > 1) return launch_sum_partials(a_parts, a_splits, (int)M, epi.a_sums, stream);
     if (e != cudaSuccess || p.splits == 1) return e;
     const long long quads = M * ((N + 3) / 4), need = (quads + 255) / 256, fit = 8ll * sm_count;
