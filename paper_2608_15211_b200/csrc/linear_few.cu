@@ -63,6 +63,7 @@ __global__ void __launch_bounds__(32 * kWarps) linear_few_kernel(const LinearEpi
     for (int o = 0; o < kOut; ++o)
 #pragma unroll
         for (int r = 0; r < R; ++r) acc[o][r] = 0;
+    let_dependents_start();
     wait_for_prerequisites();
 #pragma unroll (R >= 4 ? 2 : 4)
     for (int k = (part * 32 + lane) * V; k < n_in; k += share * 32 * V) {
@@ -120,10 +121,11 @@ auto kernel_for(int n_in) {
 cudaError_t launch_linear_few(bool e4m3, int rows, int n_in, int n_out, const void* x, const void* w, const LinearEpilogue& epi, cudaStream_t stream) {
     const int R = rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : 8, out = R == 8 ? 2 : 4;
     const int wide = e4m3 ? 16 : 8, mid = e4m3 ? 4 : 2, v = n_in % wide == 0 ? wide : n_in % mid == 0 ? mid : 1;
-    // warps that share a sum: as few as fill the device with 24 warps an SM, so that each has many runs (2 x 4096 -> 8192: 2 warps to a sum)
+    // warps that share a sum: as many as fit the device at a time (24 an SM, for one row 40), so that each has many runs and none waits for a place
+    // (4096 -> 8192: 2 rows with one warp to a sum 17.1 us, with two 18.6; 8192 -> 8192: 1 row with one warp 29.5, with two 24.2)
     const int sums = (n_out + out - 1) / out;
     int share = 1;
-    while (share < kWarps && share * 32 * v < n_in && (long long)sums * share < 24ll * kPlanSms) share *= 2;
+    while (share < kWarps && share * 32 * v < n_in && 2ll * sums * share <= (R == 1 ? 40ll : 24ll) * kPlanSms) share *= 2;
     const int per_block = kWarps / share * out;
     auto kern = e4m3 ? (R == 1 ? kernel_for<true, 1>(n_in) : R == 2 ? kernel_for<true, 2>(n_in) : R == 4 ? kernel_for<true, 4>(n_in) : kernel_for<true, 8>(n_in))
                      : (R == 1 ? kernel_for<false, 1>(n_in) : R == 2 ? kernel_for<false, 2>(n_in) : R == 4 ? kernel_for<false, 4>(n_in) : kernel_for<false, 8>(n_in));
