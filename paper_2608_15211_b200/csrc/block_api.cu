@@ -209,7 +209,12 @@ static LinearPlan make_plan(int kind, bool e4m3, long long M, int N, long long K
             }
         }
     }
-    best.group = 8;
+    // Rows of tiles that are worked on together: 8 (e4m3 156672 x 4096 -> 16384 over seconds, us: 8 8900, 4 9110; 4096 -> 4096 3892 / 3860), or down to 4
+    // where that leaves no empty units in the last group: they would make a second round of one (550800 rows, weight gradient 384 x 1536: 572 -> 1009).
+    best.group = best.m_tiles < 8 ? best.m_tiles : 0;
+    for (int g = 8; !best.group && g >= 4; --g)
+        if (best.m_tiles % g == 0) best.group = g;
+    if (!best.group) best.group = (long long)best.m_tiles * best.n_tiles * best.splits > 16 * kPlanSms ? 8 : 1;
     return best;
 }
 

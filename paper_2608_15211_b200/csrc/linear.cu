@@ -7,7 +7,7 @@
 //
 // Persistent: a unit is one output tile (of one part of the sum, where it is split).  PAIR: two CTAs on neighbouring SMs work on a
 // tile of 256 rows with tcgen05.mma.cta_group::2, each with its 128 rows of A and half of the columns of B; alone, a CTA has 128 rows.  Five
-// stages of 64 k (128 in e4m3) each, two accumulators in TMEM, so that the epilogue of a tile runs under the products of the next.
+// (or three) stages of 64 k (128 in e4m3) each, two accumulators in TMEM, so that the epilogue of a tile runs under the products of the next.
 // The epilogue works on a warp's 32 rows x 64 columns at a time, a row to a thread, two columns to an instruction; the residual comes and the
 // results go as tiles in shared memory that the copy engine moves (rows that are no multiples of 16 bytes: the warp itself, in whole rows).
 //
@@ -47,15 +47,18 @@ template <int KIND> struct Roles {
     static constexpr int kRegsLaunch = 96, kRegsEpi = 104, kRegsOther = 64;
     static_assert(kEpiWarps * kRegsEpi + kEpiWarp0 * kRegsOther <= (kEpiWarps + kEpiWarp0) * kRegsLaunch, "register hand-over does not balance");
 };
-constexpr int kStages = 5;
 constexpr int kOperand = 128 * 128;                    // bytes of an operand's stage: 128 rows (or columns) x 128 bytes
 constexpr int kTile = 32 * 128;                        // a warp's 32 rows x 64 columns of 16-bit elements, or 32 columns of 32-bit ones
-constexpr int kOffTiles = kStages * 2 * kOperand;
-constexpr int kOffBars = kOffTiles + kEpiWarpsMost * kTile;
-constexpr int kBFull = 0, kBEmpty = kStages, kBAccFull = 2 * kStages, kBAccEmpty = kBAccFull + 2, kBIn = kBAccEmpty + 2,
-              kBUsed = kBIn + kEpiWarpsMost, kBCount = kBUsed + kStages;
+// Shared memory: five stages and a tile for each epilogue warp, or, for short sums whose epilogue is the longer part, three stages and two tiles
+template <int TILES> struct Stages { static constexpr int value = TILES == 2 ? 3 : 5; };
+constexpr int kMostStages = 5;
+constexpr int kOffBars = kMostStages * 2 * kOperand + kEpiWarpsMost * kTile;
+static_assert(Stages<2>::value * 2 * kOperand + 2 * kEpiWarpsMost * kTile <= kOffBars, "the two layouts share their end");
+constexpr int kBFull = 0, kBEmpty = kMostStages, kBAccFull = 2 * kMostStages, kBAccEmpty = kBAccFull + 2, kBIn = kBAccEmpty + 2,
+              kBUsed = kBIn + 2 * kEpiWarpsMost, kBCount = kBUsed + kMostStages;
 constexpr int kOffTmem = kOffBars + 8 * kBCount, kOffAbort = kOffTmem + 4;
 constexpr int kSmem = kOffAbort + 4 + 1024;            // the base is rounded up to 1 KB
+constexpr int kTwoTilesBlocks = 8;
 constexpr int kAccCols = 256;                          // TMEM columns between the two accumulators
 
 // ---- two CTAs on one tile --------------------------------------------------------------------------------------
@@ -255,8 +258,8 @@ __device__ __forceinline__ void copy_tile(uint32_t tile, bool narrow, uint16_t* 
 }
 
 // 32 columns of a thread's row: out of TMEM (`acc`), through the epilogue, into the warp's tile from its 16-byte place `first` on.
-// IN: the places that take y hold the residual or z_in before.  Z: z goes 2 KB behind.
-template <int KIND, int ACT, bool E4M3, bool IN, bool Z>
+// IN: the places that take y hold the residual or z_in before.  Z: z goes 2 KB behind, or (WIDE) into the next tile.
+template <int KIND, int ACT, bool E4M3, bool IN, bool Z, bool WIDE>
 __device__ __forceinline__ void finish32(const uint32_t (&acc)[32], const LinearEpilogue& e, int n, int col, int first, int lane, float x_scale, uint32_t tile) {
 #pragma unroll
     for (int part = 0; part < 2; ++part) {
@@ -267,7 +270,7 @@ __device__ __forceinline__ void finish32(const uint32_t (&acc)[32], const Linear
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {                  // 8 columns: one 16-byte place
-            const uint32_t at = tile + place(lane, first + 2 * part + h, Z);
+            const uint32_t at = tile + place(lane, first + 2 * part + h, Z && !WIDE);
             uint32_t in[4] = {0, 0, 0, 0}, y[4], z[4];
             if (IN) asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];\n" : "=r"(in[0]), "=r"(in[1]), "=r"(in[2]), "=r"(in[3]) : "r"(at) : "memory");
 #pragma unroll
@@ -285,7 +288,7 @@ __device__ __forceinline__ void finish32(const uint32_t (&acc)[32], const Linear
             }
             asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(at), "r"(y[0]), "r"(y[1]), "r"(y[2]), "r"(y[3]) : "memory");
             if (KIND == kLinearForward && Z)
-                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(at + kTile / 2), "r"(z[0]), "r"(z[1]), "r"(z[2]), "r"(z[3]) : "memory");
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(at + (WIDE ? kTile : kTile / 2)), "r"(z[0]), "r"(z[1]), "r"(z[2]), "r"(z[3]) : "memory");
         }
     }
 }
@@ -320,11 +323,11 @@ __device__ __forceinline__ void write_sums(uint32_t tile, float* out, long long 
 
 // MAP: the rows of the outputs (and of the residual or z_in) are multiples of 16 bytes and the copy engine moves them; else the warps do.  (One kernel with
 // both spilled registers around the warps' copies: 2203200 x 256 -> 384 558 -> 1032 us.)
-template <bool PAIR, int KIND, bool E4M3, bool MAP>
+template <bool PAIR, int KIND, bool E4M3, bool MAP, int TILES>
 __global__ void __launch_bounds__(Roles<KIND>::kThreads, 1) linear_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Job job) {
     constexpr int CTAS = PAIR ? 2 : 1;
     using R = Roles<KIND>;
-    constexpr int kEpiWarps = R::kEpiWarps, kGroups = R::kGroups;
+    constexpr int kEpiWarps = R::kEpiWarps, kGroups = R::kGroups, kStages = Stages<TILES>::value, kOffTiles = kStages * 2 * kOperand;
     constexpr int kTileRows = 128 * CTAS;
     constexpr bool A_MN = KIND == kLinearWeights, B_MN = KIND != kLinearForward;
     constexpr int kBK = E4M3 ? 128 : 64;               // elements of a stage along k
@@ -345,7 +348,7 @@ __global__ void __launch_bounds__(Roles<KIND>::kThreads, 1) linear_kernel(const 
             mbar_init(bar(kBAccFull + b), 1);
             mbar_init(bar(kBAccEmpty + b), kEpiWarps * CTAS);
         }
-        for (int w = 0; w < kEpiWarps; ++w) mbar_init(bar(kBIn + w), 1);
+        for (int w = 0; w < 2 * kEpiWarps; ++w) mbar_init(bar(kBIn + w), 1);
         *cta_abort = 0;
         fence_barrier_init();
     }
@@ -500,7 +503,7 @@ __global__ void __launch_bounds__(Roles<KIND>::kThreads, 1) linear_kernel(const 
         // A chunk is 64 columns of the warp's 32 rows.  The chunks of all tiles go to the groups of four warps in turn: a warp has one or two of a tile,
         // or none of a narrow one.  (Every warp waits for every accumulator and gives it back, so that none falls behind by a phase.)
         const int quarter = warp & 3, group = (warp - kEpiWarp0) >> 2, chunks = (job.bn + 63) >> 6;
-        const uint32_t tile = base + kOffTiles + (warp - kEpiWarp0) * kTile;
+        const uint32_t tile = base + kOffTiles + (warp - kEpiWarp0) * TILES * kTile;
         const uint32_t lane_tmem = tmem + ((uint32_t)(quarter * 32) << 16);
         uint32_t done = 0;
         bool ok = true;
@@ -581,32 +584,40 @@ __global__ void __launch_bounds__(Roles<KIND>::kThreads, 1) linear_kernel(const 
                 next_chunk();
             }
         } else {
-            // The tile takes the residual (or z_in) first and y over it, each thread its row.  With z a chunk goes in two pieces of 32 columns, y in the
-            // first 2 KB of the tile and z in the others.
+            // A tile takes the residual (or z_in) first and y over it, each thread its row.  One tile: with z a chunk goes in two pieces of 32 columns, y in
+            // the first 2 KB of the tile and z in the others.  Two tiles: z has the second, or else the chunks take them in turn, and the next chunk's
+            // residual comes while this one is worked on.
             const void* in = KIND == kLinearForward ? job.e.residual : job.e.z_in;
             const bool has_in = in != nullptr, has_z = KIND == kLinearForward && !E4M3 && job.e.z != nullptr;
-            const int width = has_z ? 32 : 64;
-            const uint32_t in_bar = bar(kBIn + warp - kEpiWarp0);
-            uint32_t n_in = 0;                         // tiles that the copy engine brought
+            const bool fetched = MAP && has_in;
+            const int width = TILES == 1 && has_z ? 32 : 64;
+            uint32_t taken = 0;                        // tiles that took a residual by the copy engine; two tiles: chunks
+            bool ahead = false;                        // the chunk's residual is under way
+            // by one lane: waits until the tile is free and asks for the residual
+            auto prepare = [&](long long row0, int col, uint32_t t) {
+                if (TILES == 2 && !has_in && !has_z) stores_read<1>();
+                else stores_read<0>();
+                if (fetched) {
+                    const uint32_t b = bar(kBIn + TILES * (warp - kEpiWarp0) + (int)t);
+                    mbar_arrive_expect_tx(b, 64 * width);
+                    tma_load_2d(tile + t * kTile, &maps.in, col, (int)row0, b);
+                }
+            };
+            auto landed = [&](uint32_t t, volatile int* abort, long long limit) {
+                return mbar_wait<0>(bar(kBIn + TILES * (warp - kEpiWarp0) + (int)t), (TILES == 2 ? taken >> 1 : taken) & 1, abort, limit);
+            };
+            // whether this group has a chunk of a unit
+            auto has_chunk = [&](const Units& u, int chunk) { return chunk < chunks && u.n0() + 64 * chunk < job.N && u.m0(kTileRows) + 128 * rank + 32 * quarter < job.M; };
             for (; at.there() && ok; at.next(), ++done) {
                 const long long row0 = at.m0(kTileRows) + 128 * rank + 32 * quarter;
                 const int n0 = at.n0();
                 const uint32_t buf = done & 1, acc = lane_tmem + buf * kAccCols;
                 const int rows = (int)min(32ll, job.M - row0);
-                // (rows <= 0: the tile's last rows are no rows)
-                const bool fetched = MAP && has_in;
-                auto prepare = [&](int col) {          // by one lane
-                    stores_read<0>();                  // the tile is free
-                    if (fetched) {
-                        mbar_arrive_expect_tx(in_bar, 64 * width);
-                        tma_load_2d(tile, &maps.in, col, (int)row0, in_bar);
-                    }
-                };
-                bool mine = false;                     // the residual comes while the accumulator is waited for
-                if (first_chunk < chunks && rows > 0 && n0 + 64 * first_chunk < job.N) {
-                    mine = true;
+                const uint32_t t = TILES == 2 && !has_z ? taken & 1 : 0, to = tile + t * kTile;
+                const bool mine = has_chunk(at, first_chunk);
+                if (mine) {                            // the residual comes while the accumulator is waited for
                     const int c = n0 + 64 * first_chunk;
-                    if (lane == 0) prepare(c);
+                    if (lane == 0 && !ahead) prepare(row0, c, t);
                     // (the bias of the chunk: from HBM, it took longer than the rest of a small product's epilogue)
                     if (KIND == kLinearForward && lane < 2 && c + 32 * lane < job.N) {
                         if (job.e.bias) prefetch_l1(job.e.bias + c + 32 * lane);
@@ -615,39 +626,50 @@ __global__ void __launch_bounds__(Roles<KIND>::kThreads, 1) linear_kernel(const 
                 }
                 ok = wait_asleep(bar(kBAccFull + buf), (done >> 1) & 1, cta_abort);
                 if (!ok) {
-                    if (mine && fetched && lane == 0) {       // it lands before this CTA ends
+                    if (mine && fetched && lane == 0) {        // it lands before this CTA ends
                         volatile int ignore = 0;
-                        mbar_wait<0>(in_bar, n_in & 1, &ignore, 200000000LL);
+                        landed(t, &ignore, 200000000LL);
                     }
                     break;
                 }
                 tc_fence_after();
                 bool given = false;
-                if (const int chunk = first_chunk; mine) {       // (as many groups as chunks: a group has one at most)
+                if (const int chunk = first_chunk; mine) {     // (as many groups as chunks: a group has one at most)
                     const int col0 = 64 * chunk, col = n0 + col0, cols = min(64, job.bn - col0), own = min(cols, job.N - col);
-                    uint32_t cur[32];
-                    tmem_ld32(acc + col0, cur);
                     float x_scale = 1.f;
                     if (E4M3 && lane < rows) x_scale = __ldg(job.e.x_scale + row0 + lane);
 #pragma unroll 1
                     for (int p0 = 0; p0 < cols; p0 += 32) {
-                        if (p0 > 0) tmem_ld32(acc + col0 + p0, cur);
-                        if (p0 == 0 || has_z) {        // a new tile
-                            if (lane == 0 && p0 > 0) prepare(col + p0);
+                        if (p0 == 0 || width == 32) {          // a new tile
+                            if (lane == 0 && p0 > 0) prepare(row0, col + p0, t);
                             __syncwarp();
                             if (fetched) {
-                                ok = mbar_wait_all(in_bar, n_in & 1, cta_abort);
+                                ok = __all_sync(0xffffffffu, landed(t, cta_abort, 4000000000LL));
                                 if (!ok) {
                                     volatile int ignore = 0;
-                                    if (lane == 0) mbar_wait<0>(in_bar, n_in & 1, &ignore, 200000000LL);
+                                    if (lane == 0) landed(t, &ignore, 200000000LL);
                                     break;
                                 }
-                                ++n_in;
+                                if (TILES == 1) ++taken;
                             } else if (!MAP && has_in) {
-                                if (own > p0) copy_tile<false>(tile, has_z, (uint16_t*)in + row0 * job.N + col + p0, job.N, rows, min(width, own - p0), lane);
+                                if (own > p0) copy_tile<false>(to, width == 32, (uint16_t*)in + row0 * job.N + col + p0, job.N, rows, min(width, own - p0), lane);
                                 __syncwarp();
                             }
+                            if (TILES == 2 && fetched) {       // the next chunk's
+                                Units next = at;
+                                int c = first_chunk;
+                                do {
+                                    next.next();
+                                    c -= chunks;
+                                    while (c < 0) c += kGroups;
+                                } while (next.there() && !has_chunk(next, c));
+                                ahead = next.there();
+                                ++taken;
+                                if (ahead && lane == 0) prepare(next.m0(kTileRows) + 128 * rank + 32 * quarter, next.n0() + 64 * c, t ^ 1);
+                            }
                         }
+                        uint32_t cur[32];
+                        tmem_ld32(acc + col0 + p0, cur);
                         tmem_ld_wait();
                         if (p0 + 32 >= cols) {         // the accumulator has been read
                             give_back(buf);
@@ -655,34 +677,40 @@ __global__ void __launch_bounds__(Roles<KIND>::kThreads, 1) linear_kernel(const 
                         }
                         with_act(job.e.activation, [&](auto tag) {
                             constexpr int ACT = decltype(tag)::value;
-                            if (has_z && has_in) finish32<KIND, ACT, E4M3, true, true>(cur, job.e, job.N, col + p0, 0, lane, x_scale, tile);
-                            else if (has_z) finish32<KIND, ACT, E4M3, false, true>(cur, job.e, job.N, col + p0, 0, lane, x_scale, tile);
-                            else if (has_in) finish32<KIND, ACT, E4M3, true, false>(cur, job.e, job.N, col + p0, p0 >> 3, lane, x_scale, tile);
-                            else finish32<KIND, ACT, E4M3, false, false>(cur, job.e, job.N, col + p0, p0 >> 3, lane, x_scale, tile);
+                            constexpr bool W = TILES == 2;
+                            if (TILES == 1 && has_z && has_in) finish32<KIND, ACT, E4M3, true, true, W>(cur, job.e, job.N, col + p0, 0, lane, x_scale, to);
+                            else if (has_z) finish32<KIND, ACT, E4M3, false, true, W>(cur, job.e, job.N, col + p0, W ? p0 >> 3 : 0, lane, x_scale, to);
+                            else if (has_in) finish32<KIND, ACT, E4M3, true, false, W>(cur, job.e, job.N, col + p0, p0 >> 3, lane, x_scale, to);
+                            else finish32<KIND, ACT, E4M3, false, false, W>(cur, job.e, job.N, col + p0, p0 >> 3, lane, x_scale, to);
                         });
-                        if (!has_z && p0 + 32 < cols) continue;
-                        const int at = has_z ? p0 : 0; // the tile's first column
+                        if (width == 64 && p0 + 32 < cols) continue;
+                        const int at0 = width == 32 ? p0 : 0;  // the tile's first column
                         if (MAP) {
                             fence_proxy_async();
                             __syncwarp();
                             if (lane == 0) {
-                                store_box(&maps.y, col + at, (int)row0, tile);
-                                if (has_z) store_box(&maps.z, col + at, (int)row0, tile + kTile / 2);
+                                store_box(&maps.y, col + at0, (int)row0, to);
+                                if (has_z) store_box(&maps.z, col + at0, (int)row0, to + (TILES == 2 ? kTile : kTile / 2));
                                 stores_commit();
                             }
                         } else {
                             __syncwarp();
-                            if (own > at) {
-                                const long long where = row0 * job.N + col + at;
-                                copy_tile<true>(tile, has_z, (uint16_t*)job.e.y + where, job.N, rows, min(width, own - at), lane);
-                                if (has_z) copy_tile<true>(tile + kTile / 2, true, (uint16_t*)job.e.z + where, job.N, rows, min(width, own - at), lane);
+                            if (own > at0) {
+                                const long long where = row0 * job.N + col + at0;
+                                copy_tile<true>(to, width == 32, (uint16_t*)job.e.y + where, job.N, rows, min(width, own - at0), lane);
+                                if (has_z) copy_tile<true>(to + kTile / 2, true, (uint16_t*)job.e.z + where, job.N, rows, min(width, own - at0), lane);
                             }
                             __syncwarp();
                         }
                     }
+                    if (TILES == 2 && !fetched) ++taken;
                 }
-                if (ok && !given) give_back(buf);      // a warp without a chunk here, or whose last one has no rows or columns
+                if (ok && !given) give_back(buf);      // a warp without a chunk here
                 next_chunk();
+            }
+            if (!ok && ahead && lane == 0) {           // what was asked for ahead lands before this CTA ends
+                volatile int ignore = 0;
+                landed(taken & 1, &ignore, 200000000LL);
             }
             if (lane == 0) stores_read<0>();
             __syncwarp();
@@ -805,9 +833,9 @@ bool encode_map(CUtensorMap* map, const void* base, long long fast, long long sl
                CU_TENSOR_MAP_INTERLEAVE_NONE, box_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <bool PAIR, int KIND, bool E4M3, bool MAP>
+template <bool PAIR, int KIND, bool E4M3, bool MAP, int TILES>
 cudaError_t launch_one(const Maps& maps, Job& job, int sm_count, cudaStream_t stream) {
-    auto kern = linear_kernel<PAIR, KIND, E4M3, MAP>;
+    auto kern = linear_kernel<PAIR, KIND, E4M3, MAP, TILES>;
     cudaError_t e = prepare_kernel((const void*)kern, kSmem);
     if (e != cudaSuccess) return e;
     const unsigned units = (unsigned)(job.groups * job.group * job.n_tiles * job.splits), fit = (unsigned)sm_count / (PAIR ? 2 : 1), at_a_time = units < fit ? units : fit;
@@ -833,9 +861,11 @@ cudaError_t launch_one(const Maps& maps, Job& job, int sm_count, cudaStream_t st
 }
 
 template <int KIND, bool E4M3>
-cudaError_t launch_kind(bool pair, bool map, const Maps& maps, Job& job, int sm_count, cudaStream_t stream) {
-    if (pair) return map ? launch_one<true, KIND, E4M3, true>(maps, job, sm_count, stream) : launch_one<true, KIND, E4M3, false>(maps, job, sm_count, stream);
-    return map ? launch_one<false, KIND, E4M3, true>(maps, job, sm_count, stream) : launch_one<false, KIND, E4M3, false>(maps, job, sm_count, stream);
+cudaError_t launch_kind(bool pair, bool map, int tiles, const Maps& maps, Job& job, int sm_count, cudaStream_t stream) {
+    if constexpr (!E4M3)
+        if (pair && tiles == 2) return launch_one<true, KIND, E4M3, true, 2>(maps, job, sm_count, stream);
+    if (pair) return map ? launch_one<true, KIND, E4M3, true, 1>(maps, job, sm_count, stream) : launch_one<true, KIND, E4M3, false, 1>(maps, job, sm_count, stream);
+    return map ? launch_one<false, KIND, E4M3, true, 1>(maps, job, sm_count, stream) : launch_one<false, KIND, E4M3, false, 1>(maps, job, sm_count, stream);
 }
 
 }  // namespace
@@ -860,7 +890,11 @@ cudaError_t launch_linear(int kind, bool e4m3, const LinearPlan& p, long long M,
     const void* in = kind == kLinearForward ? epi.residual : epi.z_in;
     const bool by_map = kind != kLinearWeights && p.splits == 1 && N % 8 == 0;
     maps.in = maps.y = maps.z = maps.a;
-    const int wide = epi.z ? 64 : 128;
+    // Two tiles a warp where the epilogue takes longer than the products: short sums with a residual or z_in to read or a costly activation.  One tile / two, us:
+    // 550800 x 384 -> 1536, residual 802 / 760, silu 818 / 698, gelu with z 1078 / 1020, d_x of silu 1016 / 830; but z alone 798 / 850, e4m3 with gelu
+    // 1029 / 1090; 131072 x 768 -> 768, d_x of gelu 183 / 203.
+    const bool costly = in || epi.activation >= TERRA_ACT_SILU;
+    const int tiles = by_map && p.pair && !e4m3 && p.k_blocks <= kTwoTilesBlocks && costly && !(in && epi.z) ? 2 : 1, wide = epi.z && tiles == 1 ? 64 : 128;
     if (by_map && ((in && !encode_map(&maps.in, in, N, M, 2ll * N, 2, 32, wide)) || !encode_map(&maps.y, epi.y, N, M, 2ll * N, 2, 32, wide) ||
                    (epi.z && !encode_map(&maps.z, epi.z, N, M, 2ll * N, 2, 32, wide))))
         return cudaErrorInvalidValue;
@@ -890,10 +924,10 @@ cudaError_t launch_linear(int kind, bool e4m3, const LinearPlan& p, long long M,
     // (a part of a split sum goes neither way)
     const bool map = by_map || p.splits > 1;
     cudaError_t e;
-    if (kind == kLinearForward && e4m3) e = launch_kind<kLinearForward, true>(p.pair, map, maps, job, sm_count, stream);
-    else if (kind == kLinearForward) e = launch_kind<kLinearForward, false>(p.pair, map, maps, job, sm_count, stream);
-    else if (kind == kLinearInput) e = launch_kind<kLinearInput, false>(p.pair, map, maps, job, sm_count, stream);
-    else e = p.pair ? launch_one<true, kLinearWeights, false, true>(maps, job, sm_count, stream) : launch_one<false, kLinearWeights, false, true>(maps, job, sm_count, stream);
+    if (kind == kLinearForward && e4m3) e = launch_kind<kLinearForward, true>(p.pair, map, tiles, maps, job, sm_count, stream);
+    else if (kind == kLinearForward) e = launch_kind<kLinearForward, false>(p.pair, map, tiles, maps, job, sm_count, stream);
+    else if (kind == kLinearInput) e = launch_kind<kLinearInput, false>(p.pair, map, tiles, maps, job, sm_count, stream);
+    else e = p.pair ? launch_one<true, kLinearWeights, false, true, 1>(maps, job, sm_count, stream) : launch_one<false, kLinearWeights, false, true, 1>(maps, job, sm_count, stream);
     if (e == cudaSuccess && p.splits == 1 && a_splits > 1) return launch_sum_partials(a_parts, a_splits, (int)M, epi.a_sums, stream);
     if (e != cudaSuccess || p.splits == 1) return e;
     const long long quads = M * ((N + 3) / 4), need = (quads + 255) / 256, fit = 8ll * sm_count;
