@@ -300,7 +300,7 @@ def _code(names: dict, name: str, what: str) -> int:
 
 def terra_rms_norm_fwd(x, weight, residual=None, eps=1e-6, h=None, y=None, rstd=None):
     """h = x + residual, y = h weight / sqrt(mean(h^2) + eps) over the last dimension.  x, residual bf16 or fp16 [..., channels]; weight fp32
-    [channels].  Returns (y like x, h like x, rstd fp32 [rows]); without a residual h is x itself."""
+    [channels].  Returns (y like x, h like x, rstd fp32 [rows]); without a residual h is x itself (None where y was written over it)."""
     return (_host or _native()).norm_fwd(x, weight, residual, eps, h, y, rstd)
 
 

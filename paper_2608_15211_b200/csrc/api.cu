@@ -408,7 +408,7 @@ const char* terra_strerror(int status) {
     switch (status) {
         case TERRA_OK: return "ok";
         case TERRA_ERR_INVALID_ARG: return "invalid argument (null pointer, non-positive size, or size out of range)";
-        case TERRA_ERR_UNSUPPORTED: return "unsupported configuration (head_dim must be 32, 64 or 128, window <= 128, GPU must be sm_100)";
+        case TERRA_ERR_UNSUPPORTED: return "unsupported configuration (head_dim must be 32, 64 or 128, window <= 128, norm channels <= 16384, product features <= 65536, GPU must be sm_100)";
         case TERRA_ERR_ALIGNMENT: return "pointer is not 16-byte aligned";
         case TERRA_ERR_WORKSPACE: return "workspace missing or too small (see terra_swin_workspace_bytes)";
         case TERRA_ERR_CUDA: return "CUDA error (see terra_last_cuda_error)";

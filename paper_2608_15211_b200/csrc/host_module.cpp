@@ -362,7 +362,8 @@ PyObject* norm_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
         at::Tensor y = result(a[5], "y", x.scalar_type(), x.sizes(), x);
         at::Tensor rstd = result(a[6], "rstd", at::kFloat, {d.rows}, x);
         launch(f_norm_fwd, &d, px, pr, (const float*)pw, opt_ptr(h), ptr(y), (float*)ptr(rstd), stream());
-        return tuple({y, h.defined() ? h : x, rstd});
+        if (!h.defined() && ptr(y) != px) h = x;
+        return tuple_opt({y, h, rstd});
     });
 }
 

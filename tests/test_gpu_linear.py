@@ -105,9 +105,10 @@ def test_eight_bit_operands():
     held("y", y, act(z, "gelu"), 1.2 * off + z.abs() * 1.2e-5, F16)
 
 
-def test_rows_do_not_meet_and_given_buffers():
-    g = gen("rows")
-    x, w, r = ints(g, 300, 72), ints(g, 100, 72), ints(g, 300, 100)
+@pytest.mark.parametrize("n_in,n_out", [(72, 100), (128, 256), (256, 96), (1024, 320)])      # rows by the warps; by the copy engine, two tiles a warp and one
+def test_rows_do_not_meet_and_given_buffers(n_in, n_out):
+    g = gen("rows", n_in)
+    x, w, r = ints(g, 300, n_in), ints(g, n_out, n_in), ints(g, 300, n_out)
     y, z = terra.terra_linear_fwd(x, w, residual=r, activation="gelu", keep_z=True)
     bad = x.clone()
     bad[17], bad[299, 3] = float("nan"), float("inf")
@@ -117,10 +118,10 @@ def test_rows_do_not_meet_and_given_buffers():
     over = r.clone()
     y2, z2 = terra.terra_linear_fwd(x, w, residual=over, activation="gelu", y=over, z=torch.empty_like(r))
     assert y2.data_ptr() == over.data_ptr() and torch.equal(over, y) and torch.equal(z2, z)
-    dz, z_in = ints(g, 300, 100), ints(g, 300, 72)
+    dz, z_in = ints(g, 300, n_out), ints(g, 300, n_in)
     dx, dw, db = terra.terra_linear_bwd(x, w, dz, z_in=z_in, activation="silu")
     over = z_in.clone()
-    ws = torch.empty(terra.terra_linear_workspace_bytes(300, 72, 100, "bwd"), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(terra.terra_linear_workspace_bytes(300, n_in, n_out, "bwd"), dtype=torch.uint8, device="cuda")
     got = terra.terra_linear_bwd(x, w, dz, z_in=over, activation="silu", d_x=over, d_w=torch.empty_like(dw), d_bias=torch.empty_like(db), workspace=ws)
     assert got[0].data_ptr() == over.data_ptr() and all(torch.equal(a, b) for a, b in zip(got, (dx, dw, db)))
 

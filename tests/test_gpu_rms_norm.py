@@ -96,6 +96,10 @@ def test_outputs_over_inputs_and_given_buffers():
     x2, r2 = x.clone(), r.clone()
     y2, h2, _ = terra.terra_rms_norm_fwd(x2, w, residual=r2, h=r2, y=x2)
     assert y2.data_ptr() == x2.data_ptr() and torch.equal(y2, y) and torch.equal(r2, h)
+    plain, _, _ = terra.terra_rms_norm_fwd(x, w)
+    x2 = x.clone()
+    y2, h2, _ = terra.terra_rms_norm_fwd(x2, w, y=x2)
+    assert torch.equal(y2, plain) and h2 is None             # the sum, x, is gone
     dx, dw = terra.terra_rms_norm_bwd(h, w, rstd, dy, d_h=dh)
     ws = torch.empty(terra.terra_rms_norm_workspace_bytes(70, 192), dtype=torch.uint8, device="cuda")
     for over in ("d_y", "d_h"):
