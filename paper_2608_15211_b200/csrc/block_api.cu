@@ -105,11 +105,11 @@ LinearLayout layout_linear(const terra_linear_desc* d, int call) {
     return l;
 }
 
-cudaError_t pad(const void*& p, bool wanted, char* to, long long rows, long long bytes, long long stride, int sms, cudaStream_t st) {
-    if (!wanted) return cudaSuccess;
-    const cudaError_t e = launch_pad_rows(p, to, rows, (int)bytes, (int)stride, sms, st);
+// `p` is to be read with rows of `stride` bytes: where they are not, from a copy at `to`
+void pad(PadJobs& jobs, const void*& p, bool wanted, char* to, long long rows, long long bytes, long long stride) {
+    if (!wanted) return;
+    jobs.job[jobs.count++] = {p, to, rows, (int)bytes, (int)stride};
     p = to;
-    return e;
 }
 
 int linear_fwd(const terra_linear_desc* d, bool e4m3, const void* x, const float* x_scale, const void* w, const float* w_scale, const float* bias, const void* residual,
@@ -135,8 +135,10 @@ int linear_fwd(const terra_linear_desc* d, bool e4m3, const void* x, const float
         auto few = d->dtype == TERRA_DTYPE_F16 ? launch_linear_few_f16 : launch_linear_few;
         return done(few(e4m3, (int)d->rows, d->n_in, d->n_out, x, w, epi, st), where);
     }
-    cudaError_t e = pad(x, l.pad_x, ws + l.off_x, d->rows, d->n_in * elem, l.stride_x, sms, st);
-    if (e == cudaSuccess) e = pad(w, l.pad_w, ws + l.off_w, d->n_out, d->n_in * elem, l.stride_w, sms, st);
+    PadJobs jobs = {};
+    pad(jobs, x, l.pad_x, ws + l.off_x, d->rows, d->n_in * elem, l.stride_x);
+    pad(jobs, w, l.pad_w, ws + l.off_w, d->n_out, d->n_in * elem, l.stride_w);
+    const cudaError_t e = jobs.count ? launch_pad_rows(jobs, sms, st) : cudaSuccess;
     if (e != cudaSuccess) return done(e, where);
     auto launch = d->dtype == TERRA_DTYPE_F16 ? launch_linear_f16 : launch_linear;
     return done(launch(kLinearForward, e4m3, l.first, d->rows, d->n_out, d->n_in, x, l.stride_x, w, l.stride_w, epi, nullptr, (float*)(ws + l.off_parts), nullptr, sms, st), where);
@@ -311,24 +313,23 @@ int terra_linear_bwd(const terra_linear_desc* desc, const void* x, const void* w
     cudaStream_t st = (cudaStream_t)stream;
     const bool f16 = desc->dtype == TERRA_DTYPE_F16;
     auto launch = f16 ? launch_linear_f16 : launch_linear;
-    cudaError_t e = pad(d_z, l.pad_z, ws + l.off_z, desc->rows, 2ll * desc->n_out, l.stride_z, sms, st);
-    // (the weight gradient first: d_x may be written over z_in, which is x's neighbour in no call, but reads stay ahead of writes)
+    PadJobs jobs = {};
+    pad(jobs, d_z, l.pad_z, ws + l.off_z, desc->rows, 2ll * desc->n_out, l.stride_z);
+    if (d_w) pad(jobs, x, l.pad_x, ws + l.off_x, desc->rows, 2ll * desc->n_in, l.stride_x);
+    if (d_x) pad(jobs, w, l.pad_w, ws + l.off_w, desc->n_out, 2ll * desc->n_in, l.stride_w);
+    cudaError_t e = jobs.count ? launch_pad_rows(jobs, sms, st) : cudaSuccess;
     if (e == cudaSuccess && d_w) {
-        e = pad(x, l.pad_x, ws + l.off_x, desc->rows, 2ll * desc->n_in, l.stride_x, sms, st);
         LinearEpilogue epi = {};
         epi.a_sums = d_bias;
-        if (e == cudaSuccess)
-            e = launch(kLinearWeights, false, l.second, desc->n_out, desc->n_in, desc->rows, d_z, l.stride_z, x, l.stride_x, epi, d_w, parts, sums, sms, st);
+        e = launch(kLinearWeights, false, l.second, desc->n_out, desc->n_in, desc->rows, d_z, l.stride_z, x, l.stride_x, epi, d_w, parts, sums, sms, st);
     } else if (e == cudaSuccess && d_bias) {
         e = f16 ? launch_column_sums_f16(d_z, desc->rows, desc->n_out, l.stride_z / 2, sums, d_bias, st)
                 : launch_column_sums(d_z, desc->rows, desc->n_out, l.stride_z / 2, sums, d_bias, st);
     }
     if (e == cudaSuccess && d_x) {
-        e = pad(w, l.pad_w, ws + l.off_w, desc->n_out, 2ll * desc->n_in, l.stride_w, sms, st);
         LinearEpilogue epi = {};
         epi.z_in = z_in; epi.y = d_x; epi.activation = z_in ? desc->activation : TERRA_ACT_NONE;
-        if (e == cudaSuccess)
-            e = launch(kLinearInput, false, l.first, desc->rows, desc->n_in, desc->n_out, d_z, l.stride_z, w, l.stride_w, epi, nullptr, parts, nullptr, sms, st);
+        e = launch(kLinearInput, false, l.first, desc->rows, desc->n_in, desc->n_out, d_z, l.stride_z, w, l.stride_w, epi, nullptr, parts, nullptr, sms, st);
     }
     return done(e, where);
 }

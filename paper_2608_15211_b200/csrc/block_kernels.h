@@ -97,8 +97,10 @@ cudaError_t read_linear_status(int* timed_out);       // after the stream has be
 cudaError_t read_linear_status_f16(int* timed_out);
 
 // ---- around the products (linear_aux.cu) ------------------------------------------------------------------------
-// rows of `bytes` into rows of `stride` bytes (a multiple of 16), zeros behind them
-cudaError_t launch_pad_rows(const void* src, void* dst, long long rows, int bytes, int stride, int sm_count, cudaStream_t stream);
+// rows of `bytes` into rows of `stride` bytes (a multiple of 16), zeros behind them; up to three tensors at once
+struct PadJob { const void* src; void* dst; long long rows; int bytes, stride; };
+struct PadJobs { PadJob job[3]; int count; };
+cudaError_t launch_pad_rows(const PadJobs& jobs, int sm_count, cudaStream_t stream);
 // out[c] = sum over the rows of x[., c]; rows of `stride` elements; `partial`: column_sum_blocks rows of `columns`
 int column_sum_blocks(long long rows, int columns);
 cudaError_t launch_column_sums(const void* x, long long rows, int columns, long long stride, float* partial, float* out, cudaStream_t stream);

@@ -729,7 +729,64 @@ __global__ void __launch_bounds__(Roles<KIND>::kThreads, 1) linear_kernel(const 
     if (tid == 0 && *cta_abort) atomicExch(&g_linear_timeout, 1);
 }
 
-// Joins the parts of a split product: the sum over the splits, then the epilogue.
+// Four columns of a joined sum, through the epilogue, to global memory.
+template <int KIND>
+__device__ __forceinline__ void join4(const LinearEpilogue& e, float (&v)[4], long long row, int col, int N, float* out) {
+    const size_t at = (size_t)row * N + col;
+    const bool wide = (N & 3) == 0;
+    if (KIND == kLinearWeights) {
+        if (wide) *reinterpret_cast<float4*>(out + at) = make_float4(v[0], v[1], v[2], v[3]);
+        else
+            for (int c = 0; c < 4; ++c)
+                if (col + c < N) out[at + c] = v[c];
+        return;
+    }
+    const uint16_t* extra = (const uint16_t*)(KIND == kLinearForward ? e.residual : e.z_in);
+    float b[4], w[4], t[4], z[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        const bool in = col + c < N;
+        b[c] = in && KIND == kLinearForward && e.bias ? e.bias[col + c] : 0.f;
+        w[c] = in && KIND == kLinearForward && e.w_scale ? e.w_scale[col + c] : 0.f;
+        t[c] = in && extra ? elem2_to_float2(extra[at + c]).x : 0.f;
+    }
+    const bool scaled = KIND == kLinearForward && e.x_scale;
+    const Pair xs = both(scaled ? e.x_scale[row] : 1.f);
+    with_act(e.activation, [&](auto tag) {
+#pragma unroll
+        for (int c = 0; c < 4; c += 2) {
+            Pair zz = 0, y;
+            const Pair d = pair_of(v[c], v[c + 1]), bb = pair_of(b[c], b[c + 1]), in = pair_of(t[c], t[c + 1]);
+            if (scaled) y = finish2<KIND, decltype(tag)::value, true>(d, bb, pmul(xs, pair_of(w[c], w[c + 1])), in, zz);
+            else y = finish2<KIND, decltype(tag)::value, false>(d, bb, 0, in, zz);
+            split_pair(y, v[c], v[c + 1]);
+            split_pair(zz, z[c], z[c + 1]);
+        }
+    });
+    if (wide) {
+        if (KIND == kLinearForward && e.z) *reinterpret_cast<uint2*>((uint16_t*)e.z + at) = make_uint2(pack_elem(z[0], z[1]), pack_elem(z[2], z[3]));
+        *reinterpret_cast<uint2*>((uint16_t*)e.y + at) = make_uint2(pack_elem(v[0], v[1]), pack_elem(v[2], v[3]));
+    } else {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            if (col + c < N) {
+                if (KIND == kLinearForward && e.z) ((uint16_t*)e.z)[at + c] = (uint16_t)pack_elem(z[c], 0.f);
+                ((uint16_t*)e.y)[at + c] = (uint16_t)pack_elem(v[c], 0.f);
+            }
+    }
+}
+__device__ __forceinline__ void part4(const float* p, int col, int N, float (&v)[4]) {       // adds four columns of a part
+    if ((N & 3) == 0) {
+        const float4 t = *reinterpret_cast<const float4*>(p);
+        v[0] += t.x; v[1] += t.y; v[2] += t.z; v[3] += t.w;
+    } else {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            if (col + c < N) v[c] += p[c];
+    }
+}
+
+// Joins the parts of a split product: the sum over the splits, in a fixed order, then the epilogue.
 template <int KIND>
 __global__ void __launch_bounds__(256) linear_join_kernel(const LinearEpilogue e, const float* __restrict__ parts, int splits, long long M, int N, float* out,
                                                           const float* __restrict__ a_parts, int a_splits) {
@@ -737,7 +794,7 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const LinearEpilogue e
     wait_for_prerequisites();
     const int per_row = (N + 3) / 4;
     const long long total = M * per_row;
-    const bool wide = (N & 3) == 0;
+    const size_t part = (size_t)M * N;
     if (KIND == kLinearWeights && a_parts)
         for (long long i = blockIdx.x * 256ll + threadIdx.x; i < M; i += gridDim.x * 256ll) {
             float v = 0.f;
@@ -749,60 +806,47 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const LinearEpilogue e
         long long row;
         int c4;
         split_item(i, per_row, row, c4);
-        const int col = 4 * c4;
-        const size_t at = (size_t)row * N + col, part = (size_t)M * N;
         float v[4] = {0.f, 0.f, 0.f, 0.f};
-        if (wide) {
 #pragma unroll 8
-            for (int s = 0; s < splits; ++s) {
-                const float4 t = *reinterpret_cast<const float4*>(parts + s * part + at);
-                v[0] += t.x; v[1] += t.y; v[2] += t.z; v[3] += t.w;
-            }
-        } else {
-            for (int s = 0; s < splits; ++s)
-                for (int c = 0; c < 4; ++c)
-                    if (col + c < N) v[c] += parts[s * part + at + c];
-        }
-        if (KIND == kLinearWeights) {
-            if (wide) *reinterpret_cast<float4*>(out + at) = make_float4(v[0], v[1], v[2], v[3]);
-            else
-                for (int c = 0; c < 4; ++c)
-                    if (col + c < N) out[at + c] = v[c];
-            continue;
-        }
-        const uint16_t* extra = (const uint16_t*)(KIND == kLinearForward ? e.residual : e.z_in);
-        float b[4], w[4], t[4], z[4];
+        for (int s = 0; s < splits; ++s) part4(parts + s * part + (size_t)row * N + 4 * c4, 4 * c4, N, v);
+        join4<KIND>(e, v, row, 4 * c4, N, out);
+    }
+}
+// The same for outputs too small to fill the device so: 8 threads share the parts of four columns.  (A thread that adds 64 parts up alone waits for
+// memory eight times.)  Blocks from `quads` on add up a_parts.
+template <int KIND>
+__global__ void __launch_bounds__(256) linear_join_small_kernel(const LinearEpilogue e, const float* __restrict__ parts, int splits, long long M, int N, float* out,
+                                                                const float* __restrict__ a_parts, int a_splits, int quads) {
+    __shared__ float sums[8][32][4];
+    let_dependents_start();
+    wait_for_prerequisites();
+    const int sub = threadIdx.x >> 5, lane = threadIdx.x & 31, per_row = (N + 3) / 4;
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    const bool is_a = KIND == kLinearWeights && (int)blockIdx.x >= quads;
+    const long long i = (is_a ? blockIdx.x - quads : blockIdx.x) * 32ll + lane;
+    long long row = 0;
+    int c4 = 0;
+    if (is_a) {
+        if (i < M)
+#pragma unroll 4
+            for (int s = sub; s < a_splits; s += 8) v[0] += a_parts[s * M + i];
+    } else if (i < M * per_row) {
+        split_item(i, per_row, row, c4);
+#pragma unroll 4
+        for (int s = sub; s < splits; s += 8) part4(parts + s * (size_t)M * N + (size_t)row * N + 4 * c4, 4 * c4, N, v);
+    }
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            const bool in = col + c < N;
-            b[c] = in && KIND == kLinearForward && e.bias ? e.bias[col + c] : 0.f;
-            w[c] = in && KIND == kLinearForward && e.w_scale ? e.w_scale[col + c] : 0.f;
-            t[c] = in && extra ? elem2_to_float2(extra[at + c]).x : 0.f;
-        }
-        const bool scaled = KIND == kLinearForward && e.x_scale;
-        const Pair xs = both(scaled ? e.x_scale[row] : 1.f);
-        with_act(e.activation, [&](auto tag) {
+    for (int c = 0; c < 4; ++c) sums[sub][lane][c] = v[c];
+    __syncthreads();
+    if (sub) return;
 #pragma unroll
-            for (int c = 0; c < 4; c += 2) {
-                Pair zz = 0, y;
-                const Pair d = pair_of(v[c], v[c + 1]), bb = pair_of(b[c], b[c + 1]), in = pair_of(t[c], t[c + 1]);
-                if (scaled) y = finish2<KIND, decltype(tag)::value, true>(d, bb, pmul(xs, pair_of(w[c], w[c + 1])), in, zz);
-                else y = finish2<KIND, decltype(tag)::value, false>(d, bb, 0, in, zz);
-                split_pair(y, v[c], v[c + 1]);
-                split_pair(zz, z[c], z[c + 1]);
-            }
-        });
-        if (wide) {
-            if (KIND == kLinearForward && e.z) *reinterpret_cast<uint2*>((uint16_t*)e.z + at) = make_uint2(pack_elem(z[0], z[1]), pack_elem(z[2], z[3]));
-            *reinterpret_cast<uint2*>((uint16_t*)e.y + at) = make_uint2(pack_elem(v[0], v[1]), pack_elem(v[2], v[3]));
-        } else {
+    for (int k = 1; k < 8; ++k)
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
-                if (col + c < N) {
-                    if (KIND == kLinearForward && e.z) ((uint16_t*)e.z)[at + c] = (uint16_t)pack_elem(z[c], 0.f);
-                    ((uint16_t*)e.y)[at + c] = (uint16_t)pack_elem(v[c], 0.f);
-                }
-        }
+        for (int c = 0; c < 4; ++c) v[c] += sums[k][lane][c];
+    if (is_a) {
+        if (i < M) e.a_sums[i] = v[0];
+    } else if (i < M * per_row) {
+        join4<KIND>(e, v, row, 4 * c4, N, out);
     }
 }
 
@@ -859,6 +903,9 @@ cudaError_t launch_one(const Maps& maps, Job& job, int sm_count, cudaStream_t st
     count_launch(stream);
     return e;
 }
+
+// where a thread for four columns leaves most of the device idle and adds up more than a few parts
+bool splits_are_many(int splits, long long quads) { return splits >= 4 && quads <= 256ll * kPlanSms; }
 
 template <int KIND, bool E4M3>
 cudaError_t launch_kind(bool pair, bool map, int tiles, const Maps& maps, Job& job, int sm_count, cudaStream_t stream) {
@@ -930,11 +977,18 @@ cudaError_t launch_linear(int kind, bool e4m3, const LinearPlan& p, long long M,
     else e = p.pair ? launch_one<true, kLinearWeights, false, true, 1>(maps, job, sm_count, stream) : launch_one<false, kLinearWeights, false, true, 1>(maps, job, sm_count, stream);
     if (e == cudaSuccess && p.splits == 1 && a_splits > 1) return launch_sum_partials(a_parts, a_splits, (int)M, epi.a_sums, stream);
     if (e != cudaSuccess || p.splits == 1) return e;
-    const long long quads = M * ((N + 3) / 4), need = (quads + 255) / 256, fit = 8ll * sm_count;
-    const unsigned grid = (unsigned)(need < fit ? need : fit);
+    const long long quads = M * ((N + 3) / 4);
+    const float* ap = a_splits ? (const float*)a_parts : nullptr;
     prof_begin("linear_join_kernel", stream);
-    auto join = kind == kLinearForward ? linear_join_kernel<kLinearForward> : kind == kLinearInput ? linear_join_kernel<kLinearInput> : linear_join_kernel<kLinearWeights>;
-    e = launch_dependent(join, grid, 256u, 0, stream, epi, (const float*)parts, p.splits, M, N, out, a_splits ? (const float*)a_parts : nullptr, a_splits);
+    if (splits_are_many(p.splits, quads)) {
+        auto join = kind == kLinearForward ? linear_join_small_kernel<kLinearForward> : kind == kLinearInput ? linear_join_small_kernel<kLinearInput> : linear_join_small_kernel<kLinearWeights>;
+        const unsigned blocks = (unsigned)((quads + 31) / 32);
+        e = launch_dependent(join, blocks + (ap ? (unsigned)((M + 31) / 32) : 0u), 256u, 0, stream, epi, (const float*)parts, p.splits, M, N, out, ap, a_splits, (int)blocks);
+    } else {
+        auto join = kind == kLinearForward ? linear_join_kernel<kLinearForward> : kind == kLinearInput ? linear_join_kernel<kLinearInput> : linear_join_kernel<kLinearWeights>;
+        const long long need = (quads + 255) / 256, fit = 8ll * sm_count;
+        e = launch_dependent(join, (unsigned)(need < fit ? need : fit), 256u, 0, stream, epi, (const float*)parts, p.splits, M, N, out, ap, a_splits);
+    }
     count_launch(stream);
     return e;
 }

@@ -14,19 +14,29 @@ namespace {
 constexpr int kBlock = 256;
 
 #ifndef TERRA_ELEM_F16
-// T: the widest unit that the source's rows are multiples of
+// T: the widest unit that all sources' rows are multiples of
 template <typename T>
-__global__ void __launch_bounds__(kBlock) pad_rows_kernel(const T* __restrict__ src, uint4* __restrict__ dst, long long total, int units, int vectors) {
+__global__ void __launch_bounds__(kBlock) pad_rows_kernel(const PadJobs jobs) {
     constexpr int kPer = 16 / sizeof(T);
-    for (long long i = blockIdx.x * (long long)kBlock + threadIdx.x; i < total; i += (long long)gridDim.x * kBlock) {
-        long long row;
-        int v;
-        split_item(i, vectors, row, v);
-        union { T t[kPer]; uint4 all; } u;
-        const T* p = src + row * units + (long long)v * kPer;
+    let_dependents_start();
+    wait_for_prerequisites();
+#pragma unroll 1
+    for (int k = 0; k < jobs.count; ++k) {
+        const PadJob& j = jobs.job[k];
+        const int units = j.bytes / (int)sizeof(T), vectors = j.stride / 16;
+        const long long total = j.rows * vectors;
+        const T* src = (const T*)j.src;
+        uint4* dst = (uint4*)j.dst;
+        for (long long i = blockIdx.x * (long long)kBlock + threadIdx.x; i < total; i += (long long)gridDim.x * kBlock) {
+            long long row;
+            int v;
+            split_item(i, vectors, row, v);
+            union { T t[kPer]; uint4 all; } u;
+            const T* p = src + row * units + (long long)v * kPer;
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) u.t[e] = v * kPer + e < units ? p[e] : T(0);
-        dst[i] = u.all;
+            for (int e = 0; e < kPer; ++e) u.t[e] = v * kPer + e < units ? p[e] : T(0);
+            dst[i] = u.all;
+        }
     }
 }
 
@@ -103,17 +113,20 @@ __global__ void __launch_bounds__(kBlock) activation_bwd_kernel(const uint16_t* 
 }  // namespace
 
 #ifndef TERRA_ELEM_F16
-cudaError_t launch_pad_rows(const void* src, void* dst, long long rows, int bytes, int stride, int sm_count, cudaStream_t stream) {
-    const int vectors = stride / 16;
-    const long long total = rows * vectors, need = (total + kBlock - 1) / kBlock, fit = 16ll * sm_count;
-    const unsigned grid = (unsigned)(need < fit ? need : fit);
+cudaError_t launch_pad_rows(const PadJobs& jobs, int sm_count, cudaStream_t stream) {
+    long long most = 0;
+    int all = 0;
+    for (int k = 0; k < jobs.count; ++k) {
+        const long long total = jobs.job[k].rows * (jobs.job[k].stride / 16);
+        most = total > most ? total : most;
+        all |= jobs.job[k].bytes;
+    }
+    const long long need = (most + kBlock - 1) / kBlock, fit = 16ll * sm_count;
+    auto kern = all % 8 == 0 ? pad_rows_kernel<unsigned long long> : all % 4 == 0 ? pad_rows_kernel<uint32_t> : all % 2 == 0 ? pad_rows_kernel<uint16_t> : pad_rows_kernel<uint8_t>;
     prof_begin("pad_rows_kernel", stream);
-    if (bytes % 8 == 0) pad_rows_kernel<unsigned long long><<<grid, kBlock, 0, stream>>>((const unsigned long long*)src, (uint4*)dst, total, bytes / 8, vectors);
-    else if (bytes % 4 == 0) pad_rows_kernel<uint32_t><<<grid, kBlock, 0, stream>>>((const uint32_t*)src, (uint4*)dst, total, bytes / 4, vectors);
-    else if (bytes % 2 == 0) pad_rows_kernel<uint16_t><<<grid, kBlock, 0, stream>>>((const uint16_t*)src, (uint4*)dst, total, bytes / 2, vectors);
-    else pad_rows_kernel<uint8_t><<<grid, kBlock, 0, stream>>>((const uint8_t*)src, (uint4*)dst, total, bytes, vectors);
+    const cudaError_t e = launch_dependent(kern, (unsigned)(need < fit ? need : fit), (unsigned)kBlock, 0, stream, jobs);
     count_launch(stream);
-    return cudaGetLastError();
+    return e;
 }
 
 int column_sum_blocks(long long rows, int columns) {
