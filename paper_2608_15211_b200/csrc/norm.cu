@@ -7,6 +7,7 @@
 // under way while a row is worked on; the weights stay in registers.  All sums in fp32.
 #include <cuda_fp8.h>
 
+#include "block_act.cuh"
 #include "block_kernels.h"
 
 #ifdef TERRA_ELEM_F16
@@ -32,18 +33,26 @@ template <> struct Raw<8> {
 #pragma unroll
         for (int i = 0; i < 4; ++i) { const float2 t = elem2_to_float2(w[i]); f[2 * i] = t.x; f[2 * i + 1] = t.y; }
     }
+    __device__ void add_to(float (&f)[8]) const {
+        add_elems(f[0], f[1], v.x);
+        add_elems(f[2], f[3], v.y);
+        add_elems(f[4], f[5], v.z);
+        add_elems(f[6], f[7], v.w);
+    }
 };
 template <> struct Raw<2> {
     uint32_t v;
     __device__ void load(const uint16_t* p) { v = *reinterpret_cast<const uint32_t*>(p); }
     __device__ void zero() { v = 0; }
     __device__ void floats(float (&f)[2]) const { const float2 t = elem2_to_float2(v); f[0] = t.x; f[1] = t.y; }
+    __device__ void add_to(float (&f)[2]) const { add_elems(f[0], f[1], v); }
 };
 template <> struct Raw<1> {
     uint32_t v;
     __device__ void load(const uint16_t* p) { v = *p; }
     __device__ void zero() { v = 0; }
     __device__ void floats(float (&f)[1]) const { f[0] = elem2_to_float2(v).x; }
+    __device__ void add_to(float (&f)[1]) const { f[0] += elem2_to_float2(v).x; }
 };
 __device__ __forceinline__ void store(uint16_t* p, const float (&f)[8]) {
     *reinterpret_cast<uint4*>(p) = make_uint4(pack_elem(f[0], f[1]), pack_elem(f[2], f[3]), pack_elem(f[4], f[5]), pack_elem(f[6], f[7]));
@@ -83,7 +92,7 @@ __device__ __forceinline__ float over_row(float s, int lanes, float* buf, int& t
     return s;
 }
 
-// What bounds it: HBM (156672 x 4096 785 us, 6.5 TB/s; e4m3 861 us, 5.2 TB/s).
+// What bounds it: HBM (156672 x 4096 785 us, 6.5 TB/s; e4m3 759 us, 5.9 TB/s).
 template <int E, int V, bool E4M3>
 __global__ void __launch_bounds__(kMaxLanes, E == 8 && V <= 2 ? 2 : 1)
 rms_norm_fwd_kernel(const NormArgs a, int lanes, int lanes_log2) {
@@ -117,7 +126,7 @@ rms_norm_fwd_kernel(const NormArgs a, int lanes, int lanes_log2) {
     };
     const long long step = (long long)gridDim.x * per_block;
     // (With the residual's reads and the sum's writes beside a 16-bit output, reads ahead make it slower: 156672 x 4096 789 -> 878 us.  Without the residual
-    // they take it from 535 to 481 us, with the output in 8 bits from 938 to 861.)
+    // they take it from 535 to 440 us, with the output in 8 bits from 938 to 861.)
     const bool ahead = E4M3 || !r;
     if (ahead) fetch((long long)blockIdx.x * per_block + sub);
     for (long long row0 = (long long)blockIdx.x * per_block; row0 < a.rows; row0 += step) {
@@ -129,12 +138,7 @@ rms_norm_fwd_kernel(const NormArgs a, int lanes, int lanes_log2) {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             xr[v].floats(f[v]);
-            if (r) {
-                float t[E];
-                rr[v].floats(t);
-#pragma unroll
-                for (int e = 0; e < E; ++e) f[v][e] += t[e];
-            }
+            if (r) rr[v].add_to(f[v]);
         }
         if (ahead) fetch(row + step);  // (rows of other blocks are not written, so outputs over inputs stay right)
 #pragma unroll
@@ -147,33 +151,47 @@ rms_norm_fwd_kernel(const NormArgs a, int lanes, int lanes_log2) {
         sum = over_row<false>(sum, lanes, buf, turn);
         const float rstd = rsqrtf(fmaf(sum, per_channel, a.eps));
         if (a.rstd && live && lane == 0) a.rstd[row] = rstd;
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-#pragma unroll
-            for (int e = 0; e < E; ++e) f[v][e] = f[v][e] * rstd * w[v][e];
         if (E4M3) {
             float top = 0.f;
 #pragma unroll
             for (int v = 0; v < V; ++v)
 #pragma unroll
-                for (int e = 0; e < E; ++e) top = max_nan(top, fabsf(f[v][e]));
-            top = over_row<true>(top, lanes, buf, turn);
+                for (int e = 0; e < E; ++e) {
+                    f[v][e] *= w[v][e];
+                    top = max_nan(top, fabsf(f[v][e]));
+                }
+            top = over_row<true>(top, lanes, buf, turn) * rstd;
             const float scale = top / kE4m3Max;
             if (live && lane == 0) a.scale[row] = scale;
-            // a row of zeros keeps its zeros; below 2^-120 the reciprocal leaves fp32's range
-            const bool by_product = !(scale < 0x1p-120f);
-            const float by = by_product ? 1.f / scale : 1.f, div = scale > 0.f ? scale : 1.f;
+            const float by = rstd / scale;             // y / scale = f weight by
+            if (scale >= 0x1p-100f && by < 0x1p100f) {
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const int c = lane + v * lanes;
+                for (int v = 0; v < V; ++v) {
+                    const int c = lane + v * lanes;
 #pragma unroll
-                for (int e = 0; e < E; ++e) f[v][e] = by_product ? f[v][e] * by : f[v][e] / div;
-                if (live && c < chunks) store_e4m3((uint8_t*)a.y + at + c * E, f[v]);
+                    for (int e = 0; e < E; ++e) f[v][e] *= by;
+                    if (live && c < chunks) store_e4m3((uint8_t*)a.y + at + c * E, f[v]);
+                }
+            } else {                                   // far out, by leaves fp32's range; a row of zeros keeps its zeros; NaN stays NaN
+                const float div = scale == 0.f ? 1.f : scale;
+#pragma unroll 1
+                for (int v = 0; v < V; ++v) {
+                    const int c = lane + v * lanes;
+#pragma unroll
+                    for (int e = 0; e < E; ++e) f[0][e] = f[0][e] * rstd / div;
+                    if (live && c < chunks) store_e4m3((uint8_t*)a.y + at + c * E, f[0]);
+#pragma unroll
+                    for (int u = 0; u + 1 < V; ++u)
+#pragma unroll
+                        for (int e = 0; e < E; ++e) f[u][e] = f[u + 1][e];
+                }
             }
         } else {
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const int c = lane + v * lanes;
+#pragma unroll
+                for (int e = 0; e < E; ++e) f[v][e] = f[v][e] * rstd * w[v][e];
                 if (live && c < chunks) store((uint16_t*)a.y + at + c * E, f[v]);
             }
         }
@@ -288,14 +306,14 @@ struct Shape { int E, V, lanes, lanes_log2, threads; };
 
 // Threads to a row: the fewest (but 4 at least) of up to `most` vectors each.  With 16-byte vectors V is the number that the row needs
 // then, so that 96, 192, 384 and 768 channels (3 vectors) leave no thread idle.  Up to 4 vectors in a warp; in rows of several warps 2, which leaves
-// registers for the next row's (156672 x 4096, with the next row ahead: forward 806 -> 785 us, e4m3 976 -> 861, backward 1661 -> 807).  Odd and even
+// registers for the next row's (156672 x 4096, with the next row ahead: forward 806 -> 785 us, e4m3 976 -> 759, backward 1661 -> 807).  Odd and even
 // numbers of channels by 2 and 4 bytes a thread: 300000 x 1001 forward 773 us, x 1002 549, x 1000 396.
 Shape shape_for(int channels, bool backward) {
     Shape s;
     s.E = channels % 8 == 0 ? 8 : channels % 2 == 0 ? 2 : 1;
     const int chunks = channels / s.E;
     int most;
-    if (s.E == 8) most = chunks > (backward ? 96 : 128) && chunks <= 1024 ? 2 : 4;
+    if (s.E == 8) most = chunks > 128 && chunks <= 1024 ? 2 : 4;
     else if (s.E == 2) most = chunks <= 8 * kMaxLanes ? 8 : 16;
     else if (backward) most = chunks <= 4 * kMaxLanes ? 4 : chunks <= 8 * kMaxLanes ? 8 : chunks <= 16 * kMaxLanes ? 16 : 32;
     else most = chunks <= 64 ? 4 : chunks <= 16 * kMaxLanes ? 16 : 32;
@@ -303,6 +321,11 @@ Shape shape_for(int channels, bool backward) {
     s.lanes_log2 = 2;
     while (s.lanes * most < chunks) { s.lanes *= 2; ++s.lanes_log2; }
     s.V = s.E == 8 ? (chunks + s.lanes - 1) / s.lanes : most;
+    if (backward && s.V == 4 && s.E == 8 && s.lanes < kMaxLanes) {        // four vectors leave no registers for the next row (300000 x 200: 151 -> 96 us)
+        s.lanes *= 2;
+        ++s.lanes_log2;
+        s.V = 2;
+    }
     s.threads = s.lanes < kBlock ? kBlock : s.lanes;
     return s;
 }
