@@ -91,16 +91,16 @@ __device__ __forceinline__ float clamp_nan(float x, float most) {
     return y;
 }
 
-// normal_tail of |x| = a (a <= 100)
-__device__ __forceinline__ void normal_tail2(Pair a, Pair& bell, Pair& tail) {
+// normal_tail of |x| = a (a <= 100), the tail negative: that is what is needed of it
+__device__ __forceinline__ void normal_tail2(Pair a, Pair& bell, Pair& minus_tail) {
     const Pair t = prcp(pfma(a, both(0.65f * 0.70710678f), both(1.f)));
     bell = pexp2(pmul(pmul(a, both(-0.5f * kLog2e)), a));
-    Pair g = pfma(both(0.5f * 0.14364023f), t, both(0.5f * -0.47167895f));
-    g = pfma(g, t, both(0.5f * 0.35566068f));
-    g = pfma(g, t, both(0.5f * 0.23218703f));
-    g = pfma(g, t, both(0.5f * 0.37380508f));
-    g = pfma(g, t, both(0.5f * 0.36639139f));
-    tail = pmul(pmul(g, t), bell);
+    Pair g = pfma(both(-0.5f * 0.14364023f), t, both(0.5f * 0.47167895f));
+    g = pfma(g, t, both(-0.5f * 0.35566068f));
+    g = pfma(g, t, both(-0.5f * 0.23218703f));
+    g = pfma(g, t, both(-0.5f * 0.37380508f));
+    g = pfma(g, t, both(-0.5f * 0.36639139f));
+    minus_tail = pmul(pmul(g, t), bell);
 }
 __device__ __forceinline__ Pair sigmoid2(Pair log2e_x) {           // of x, given x log2(e)
     float a, b;
@@ -116,9 +116,9 @@ __device__ __forceinline__ Pair act2(Pair z) {
     if (ACT == TERRA_ACT_SILU) return pmul(z, sigmoid2(pmul(z, both(kLog2e))));
     if (ACT == TERRA_ACT_GELU) {       // max(z, 0) - |z| tail; beyond 100 the tail is 0 in fp32, and |z| may be infinite
         const Pair m = pair_of(abs_upto(a, 100.f), abs_upto(b, 100.f));
-        Pair bell, tail;
-        normal_tail2(m, bell, tail);
-        return pfma(pmul(m, both(-1.f)), tail, pair_of(fmaxf(a, 0.f), fmaxf(b, 0.f)));
+        Pair bell, minus_tail;
+        normal_tail2(m, bell, minus_tail);
+        return pfma(m, minus_tail, pair_of(fmaxf(a, 0.f), fmaxf(b, 0.f)));
     }
     if (ACT == TERRA_ACT_GELU_TANH)
         return pmul(z, sigmoid2(pmul(z, pfma(pmul(z, z), both(2.f * kGeluTanhA * kLog2e * kGeluTanhB), both(2.f * kGeluTanhA * kLog2e)))));
@@ -132,13 +132,12 @@ __device__ __forceinline__ Pair act_slope2(Pair z) {
     if (ACT == TERRA_ACT_RELU) return pair_of(a > 0.f ? 1.f : 0.f, b > 0.f ? 1.f : 0.f);
     if (ACT == TERRA_ACT_GELU) {
         const Pair m = pair_of(abs_upto(a, 100.f), abs_upto(b, 100.f));
-        Pair bell, tail;
-        normal_tail2(m, bell, tail);
+        Pair bell, minus_tail;
+        normal_tail2(m, bell, minus_tail);
         // Phi(z) + z phi(z): tail - |z| phi below 0, 1 less that above
-        const Pair low = pfma(pmul(m, both(-0.3989422804f)), bell, tail);
         float u, v;
-        split_pair(low, u, v);
-        return pair_of(a < 0.f ? u : 1.f - u, b < 0.f ? v : 1.f - v);
+        split_pair(pfma(pmul(m, both(0.3989422804f)), bell, minus_tail), u, v);
+        return pair_of(a < 0.f ? -u : 1.f + u, b < 0.f ? -v : 1.f + v);
     }
     if (ACT == TERRA_ACT_SILU || ACT == TERRA_ACT_GELU_TANH) {     // beyond 100 (30 for the cube) s (1 - s) is 0 in fp32
         const Pair c = pair_of(clamp_nan(a, 100.f), clamp_nan(b, 100.f)), cc = pmul(c, c);

@@ -45,22 +45,20 @@ namespace {
 
 using namespace tc;
 
-constexpr int kEpiWarp0 = 4, kEpiWarpsMost = 16;
-// Groups of four epilogue warps, one for each 32 lanes of TMEM, and the registers of a thread at launch, in the epilogue and elsewhere
-template <int KIND> struct Roles {
-    static constexpr int kGroups = 4, kEpiWarps = 4 * kGroups, kThreads = 32 * (kEpiWarp0 + kEpiWarps);
-    static constexpr int kRegsLaunch = 96, kRegsEpi = 104, kRegsOther = 64;
-    static_assert(kEpiWarps * kRegsEpi + kEpiWarp0 * kRegsOther <= (kEpiWarps + kEpiWarp0) * kRegsLaunch, "register hand-over does not balance");
-};
+constexpr int kGroups = 4;                             // groups of four epilogue warps, one for each 32 lanes of TMEM
+constexpr int kEpiWarp0 = 4, kEpiWarps = 4 * kGroups;
+constexpr int kThreads = 32 * (kEpiWarp0 + kEpiWarps);
+constexpr int kRegsLaunch = 96, kRegsEpi = 104, kRegsOther = 64;      // of a thread at launch, in the epilogue and elsewhere
+static_assert(kEpiWarps * kRegsEpi + kEpiWarp0 * kRegsOther <= (kEpiWarps + kEpiWarp0) * kRegsLaunch, "register hand-over does not balance");
 constexpr int kOperand = 128 * 128;                    // bytes of an operand's stage: 128 rows (or columns) x 128 bytes
 constexpr int kTile = 32 * 128;                        // a warp's 32 rows x 64 columns of 16-bit elements, or 32 columns of 32-bit ones
 // Shared memory: five stages and a tile for each epilogue warp, or, for short sums whose epilogue is the longer part, three stages and two tiles
 template <int TILES> struct Stages { static constexpr int value = TILES == 2 ? 3 : 5; };
 constexpr int kMostStages = 5;
-constexpr int kOffBars = kMostStages * 2 * kOperand + kEpiWarpsMost * kTile;
-static_assert(Stages<2>::value * 2 * kOperand + 2 * kEpiWarpsMost * kTile <= kOffBars, "the two layouts share their end");
+constexpr int kOffBars = kMostStages * 2 * kOperand + kEpiWarps * kTile;
+static_assert(Stages<2>::value * 2 * kOperand + 2 * kEpiWarps * kTile <= kOffBars, "the two layouts share their end");
 constexpr int kBFull = 0, kBEmpty = kMostStages, kBAccFull = 2 * kMostStages, kBAccEmpty = kBAccFull + 2, kBIn = kBAccEmpty + 2,
-              kBUsed = kBIn + 2 * kEpiWarpsMost, kBCount = kBUsed + kMostStages;
+              kBUsed = kBIn + 2 * kEpiWarps, kBCount = kBUsed + kMostStages;
 constexpr int kOffTmem = kOffBars + 8 * kBCount, kOffAbort = kOffTmem + 4;
 constexpr int kSmem = kOffAbort + 4 + 1024;            // the base is rounded up to 1 KB
 constexpr int kTwoTilesBlocks = 8;
@@ -329,10 +327,9 @@ __device__ __forceinline__ void write_sums(uint32_t tile, float* out, long long 
 // MAP: the rows of the outputs (and of the residual or z_in) are multiples of 16 bytes and the copy engine moves them; else the warps do.  (One kernel with
 // both spilled registers around the warps' copies: 2203200 x 256 -> 384 558 -> 1032 us.)
 template <bool PAIR, int KIND, bool E4M3, bool MAP, int TILES>
-__global__ void __launch_bounds__(Roles<KIND>::kThreads, 1) linear_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Job job) {
+__global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Job job) {
     constexpr int CTAS = PAIR ? 2 : 1;
-    using R = Roles<KIND>;
-    constexpr int kEpiWarps = R::kEpiWarps, kGroups = R::kGroups, kStages = Stages<TILES>::value, kOffTiles = kStages * 2 * kOperand;
+    constexpr int kStages = Stages<TILES>::value, kOffTiles = kStages * 2 * kOperand;
     constexpr int kTileRows = 128 * CTAS;
     constexpr bool A_MN = KIND == kLinearWeights, B_MN = KIND != kLinearForward;
     constexpr int kBK = E4M3 ? 128 : 64;               // elements of a stage along k
@@ -376,7 +373,7 @@ __global__ void __launch_bounds__(Roles<KIND>::kThreads, 1) linear_kernel(const 
 
     Units at(job, blockIdx.x / CTAS);
     at.settle();
-    if (warp < kEpiWarp0) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(R::kRegsOther));
+    if (warp < kEpiWarp0) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;\n" ::"n"(kRegsOther));
     // (Warps 0 and 1 run their loops as whole warps and elect a thread for the instructions alone: what the loops count stays in the uniform
     // registers that those instructions take their operands from.  By one thread, a stage's products took 500 cycles to issue.)
     if (warp == 0) {
@@ -504,8 +501,8 @@ __global__ void __launch_bounds__(Roles<KIND>::kThreads, 1) linear_kernel(const 
         }
         __syncwarp();
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(R::kRegsEpi));
-        // A chunk is 64 columns of the warp's 32 rows.  The chunks of all tiles go to the groups of four warps in turn: a warp has one or two of a tile,
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;\n" ::"n"(kRegsEpi));
+        // A chunk is 64 columns of the warp's 32 rows.  The chunks of all tiles go to the groups of four warps in turn: a warp has one of a tile,
         // or none of a narrow one.  (Every warp waits for every accumulator and gives it back, so that none falls behind by a phase.)
         const int quarter = warp & 3, group = (warp - kEpiWarp0) >> 2, chunks = (job.bn + 63) >> 6;
         const uint32_t tile = base + kOffTiles + (warp - kEpiWarp0) * TILES * kTile;
@@ -898,7 +895,7 @@ cudaError_t launch_one(const Maps& maps, Job& job, int sm_count, cudaStream_t st
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(at_a_time * (PAIR ? 2 : 1));
-    cfg.blockDim = dim3(Roles<KIND>::kThreads);
+    cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = kSmem;
     cfg.stream = stream;
     cfg.attrs = attr;
