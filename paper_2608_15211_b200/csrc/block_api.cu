@@ -31,7 +31,7 @@ int norm_fwd(const terra_norm_desc* d, const void* x, const void* residual, cons
              const char* where) {
     int rc = check_norm(d);
     if (rc) return rc;
-    if (!x || !weight || !y || (e4m3 && !scale) || y == h) return TERRA_ERR_INVALID_ARG;
+    if (!x || !weight || !y || (e4m3 && (!scale || y == x || y == residual)) || y == h) return TERRA_ERR_INVALID_ARG;
     if (misaligned({x, residual, weight, h, y, scale, rstd})) return TERRA_ERR_ALIGNMENT;
     int sms = 0;
     rc = current_device_sm_count(&sms);
@@ -116,7 +116,8 @@ int linear_fwd(const terra_linear_desc* d, bool e4m3, const void* x, const float
                void* y, void* z, void* workspace, size_t workspace_bytes, void* stream, const char* where) {
     int rc = check_linear(d);
     if (rc) return rc;
-    if (!x || !w || !y || y == z || (e4m3 && (!x_scale || !w_scale))) return TERRA_ERR_INVALID_ARG;
+    if (!x || !w || !y || (e4m3 && (!x_scale || !w_scale))) return TERRA_ERR_INVALID_ARG;
+    if (y == z || y == x || y == w || (z && (z == x || z == w || z == residual))) return TERRA_ERR_INVALID_ARG;        // other threads still read those
     if (misaligned({x, w, x_scale, w_scale, bias, residual, y, z})) return TERRA_ERR_ALIGNMENT;
     const LinearLayout l = layout_linear(d, e4m3 ? TERRA_LINEAR_FWD_E4M3 : TERRA_LINEAR_FWD);
     if (l.bytes && (!workspace || workspace_bytes < l.bytes)) return TERRA_ERR_WORKSPACE;
@@ -156,6 +157,7 @@ int rotary(const terra_swin_desc* desc, const terra_rotary_desc* r, const double
         return TERRA_ERR_INVALID_ARG;
     if (!inv_freq || !q || !q_out || (!k != !k_out)) return TERRA_ERR_INVALID_ARG;
     if (misaligned({inv_freq, positions, q, k, q_out, k_out})) return TERRA_ERR_ALIGNMENT;
+    if (k && (q_out == k || k_out == q || q_out == k_out)) return TERRA_ERR_INVALID_ARG;
     int sms = 0;
     rc = current_device_sm_count(&sms);
     if (rc) return rc;
@@ -300,6 +302,7 @@ int terra_linear_bwd(const terra_linear_desc* desc, const void* x, const void* w
     int rc = check_linear(desc);
     if (rc) return rc;
     if (!d_z || (d_x && !w) || (d_w && !x) || (!d_x && !d_w && !d_bias)) return TERRA_ERR_INVALID_ARG;
+    if (d_x && (d_x == d_z || d_x == w)) return TERRA_ERR_INVALID_ARG;
     if (misaligned({x, w, d_z, z_in, d_x, d_w, d_bias})) return TERRA_ERR_ALIGNMENT;
     const LinearLayout l = layout_linear(desc, TERRA_LINEAR_BWD);
     if (!workspace || workspace_bytes < l.bytes) return TERRA_ERR_WORKSPACE;

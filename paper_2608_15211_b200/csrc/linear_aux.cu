@@ -87,26 +87,27 @@ __global__ void __launch_bounds__(kBlock) column_sums_kernel(const uint16_t* __r
     if (c < columns) partial[(size_t)blockIdx.y * columns + c] = all;
 }
 
-template <int E>
-__global__ void __launch_bounds__(kBlock) activation_bwd_kernel(const uint16_t* z, const uint16_t* d_y, uint16_t* d_z, long long items, int activation) {
-    for (long long i = blockIdx.x * (long long)kBlock + threadIdx.x; i < items; i += (long long)gridDim.x * kBlock) {
-        if (E == 8) {
-            const uint4 zv = *reinterpret_cast<const uint4*>(z + 8 * i), gv = *reinterpret_cast<const uint4*>(d_y + 8 * i);
-            const uint32_t zw[4] = {zv.x, zv.y, zv.z, zv.w}, gw[4] = {gv.x, gv.y, gv.z, gv.w};
-            uint32_t out[4];
-            with_act(activation, [&](auto tag) {
-                constexpr int A = decltype(tag)::value;
+// 8 elements a thread; what is behind the last 8 goes element by element to the first threads
+__global__ void __launch_bounds__(kBlock) activation_bwd_kernel(const uint16_t* z, const uint16_t* d_y, uint16_t* d_z, long long n, int activation) {
+    const long long first = blockIdx.x * (long long)kBlock + threadIdx.x, step = (long long)gridDim.x * kBlock;
+    for (long long i = first; i < n / 8; i += step) {
+        const uint4 zv = *reinterpret_cast<const uint4*>(z + 8 * i), gv = *reinterpret_cast<const uint4*>(d_y + 8 * i);
+        const uint32_t zw[4] = {zv.x, zv.y, zv.z, zv.w}, gw[4] = {gv.x, gv.y, gv.z, gv.w};
+        uint32_t out[4];
+        with_act(activation, [&](auto tag) {
+            constexpr int A = decltype(tag)::value;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float2 a = elem2_to_float2(zw[k]), g = elem2_to_float2(gw[k]);
-                    out[k] = pack_elem(g.x * act_slope<A>(a.x), g.y * act_slope<A>(a.y));
-                }
-            });
-            *reinterpret_cast<uint4*>(d_z + 8 * i) = make_uint4(out[0], out[1], out[2], out[3]);
-        } else {
-            const float a = elem2_to_float2(z[i]).x, g = elem2_to_float2(d_y[i]).x;
-            with_act(activation, [&](auto tag) { d_z[i] = (uint16_t)pack_elem(g * act_slope<decltype(tag)::value>(a), 0.f); });
-        }
+            for (int k = 0; k < 4; ++k) {
+                const float2 a = elem2_to_float2(zw[k]), g = elem2_to_float2(gw[k]);
+                out[k] = pack_elem(g.x * act_slope<A>(a.x), g.y * act_slope<A>(a.y));
+            }
+        });
+        *reinterpret_cast<uint4*>(d_z + 8 * i) = make_uint4(out[0], out[1], out[2], out[3]);
+    }
+    if (first < n % 8) {
+        const long long i = n / 8 * 8 + first;
+        const float a = elem2_to_float2(z[i]).x, g = elem2_to_float2(d_y[i]).x;
+        with_act(activation, [&](auto tag) { d_z[i] = (uint16_t)pack_elem(g * act_slope<decltype(tag)::value>(a), 0.f); });
     }
 }
 
@@ -153,12 +154,9 @@ cudaError_t launch_column_sums(const void* x, long long rows, int columns, long 
 }
 
 cudaError_t launch_activation_bwd(const void* z, const void* d_y, void* d_z, long long n, int activation, int sm_count, cudaStream_t stream) {
-    const bool wide = n % 8 == 0;
-    const long long items = wide ? n / 8 : n, need = (items + kBlock - 1) / kBlock, fit = 16ll * sm_count;
-    const unsigned grid = (unsigned)(need < fit ? need : fit);
+    const long long need = (n / 8 + kBlock) / kBlock, fit = 16ll * sm_count;        // (one thread at least behind the last 8)
     prof_begin("activation_bwd_kernel", stream);
-    if (wide) activation_bwd_kernel<8><<<grid, kBlock, 0, stream>>>((const uint16_t*)z, (const uint16_t*)d_y, (uint16_t*)d_z, items, activation);
-    else activation_bwd_kernel<1><<<grid, kBlock, 0, stream>>>((const uint16_t*)z, (const uint16_t*)d_y, (uint16_t*)d_z, items, activation);
+    activation_bwd_kernel<<<(unsigned)(need < fit ? need : fit), kBlock, 0, stream>>>((const uint16_t*)z, (const uint16_t*)d_y, (uint16_t*)d_z, n, activation);
     count_launch(stream);
     return cudaGetLastError();
 }

@@ -103,8 +103,8 @@ def test_linear_arguments(lib):
     assert lib.terra_linear_bwd(d, P, P, P, None, None, None, None, P, 1 << 30, None) == INVALID
     need = terra.terra_linear_workspace_bytes(4, 64, 32, "bwd")
     assert need > 0 and lib.terra_linear_bwd(d, *bwd, P, need - 1, None) == WORKSPACE and lib.terra_linear_bwd(d, *bwd, P + 8, need, None) == ALIGNMENT
-    odd = linear(n_in=63)
-    need = terra.terra_linear_workspace_bytes(4, 63, 32)
+    odd = linear(rows=16, n_in=63)
+    need = terra.terra_linear_workspace_bytes(16, 63, 32)
     assert need > 0 and lib.terra_linear_fwd(odd, *fwd, None, 0, None) == WORKSPACE and lib.terra_linear_fwd(odd, *fwd, P, need - 1, None) == WORKSPACE
     n = ctypes.c_size_t()
     assert lib.terra_linear_workspace_bytes(d, 3, ctypes.byref(n)) == INVALID and lib.terra_linear_workspace_bytes(d, 0, None) == INVALID
@@ -196,3 +196,18 @@ def test_rotary_frequencies():
                 dict(rot_dim=4, scaling="other")):
         with pytest.raises(ValueError):
             terra.rotary_frequencies(**bad, device="cpu")
+
+
+def test_outputs_over_inputs_that_others_still_read(lib):
+    d = linear()
+    Q, R, S = 2 * P, 3 * P, 4 * P                          # x, w, residual at P, Q, R
+    for y, z in ((P, S), (Q, S), (S, P), (S, Q), (S, R), (S, S)):
+        assert lib.terra_linear_fwd(d, P, Q, None, R, y, z, None, 0, None) == INVALID
+    for y in (P, Q):
+        assert lib.terra_linear_fwd_e4m3(d, P, S, Q, S, None, R, y, None, 0, None) == INVALID
+    for d_x in (R, Q):
+        assert lib.terra_linear_bwd(d, P, Q, R, None, d_x, S, None, P, 1 << 30, None) == INVALID
+    for y8 in (P, Q):                                      # (8 bits over 16)
+        assert lib.terra_rms_norm_fwd_e4m3(norm(), P, Q, R, None, y8, S, None, None) == INVALID
+    for q_out, k_out in ((Q, R), (R, P), (R, R)):
+        assert lib.terra_rotary(grid(), rotary(), S, None, P, Q, q_out, k_out, None) == INVALID

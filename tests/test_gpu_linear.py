@@ -142,3 +142,16 @@ def test_long_sum_over_rows():
     want = dz.double().t() @ x.double()
     assert (dw.double() - want).norm() <= 4e-6 * want.norm()
     assert (db.double() - dz.double().sum(0)).norm() <= 1e-6 * dz.double().sum(0).norm()
+
+
+@pytest.mark.parametrize("n", [1, 7, 8, 9, 2047, 2048, 2049, 2055, 16 * 148 * 2048 + 13])       # a last vector that is not whole, one block and a bit, every block twice
+def test_an_activation_alone(n):
+    g = gen("alone", n)
+    z, dy = (torch.randn(n, generator=g, device="cuda").to(BF16) for _ in range(2))
+    mem = torch.full((n + 16,), -7.0, device="cuda", dtype=BF16)
+    d_z = mem[8:8 + n]
+    assert terra.terra_activation_bwd(z, dy, "silu", d_z=d_z) is d_z
+    held("d_z", d_z, dy.double() * act_slope(z.double(), "silu"), dy.double().abs() * 2e-5, BF16)
+    assert (mem[:8] == -7).all() and (mem[8 + n:] == -7).all()
+    terra.terra_activation_bwd(z, dy, "silu", d_z=dy)       # over the gradient
+    assert torch.equal(dy, d_z)
