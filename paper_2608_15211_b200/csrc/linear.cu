@@ -18,7 +18,7 @@
 // What bounds it: the tensor pipe where the sum is long (156672 x 4096 -> 4096 3.35 ms, 1569 TFLOP/s, the pipe busy in 91 % of the cycles; e4m3 to 16384 with
 // GELU 7.2 ms, 2930 TFLOP/s), over seconds the power cap (4.1 and 9.0 ms); the epilogue where it is short (550800 x 384 -> 1536 with GELU 0.85 ms, two
 // reciprocals or exponentials an output in a unit that takes 16 a clock and SM, busy in half the cycles), with z besides the writes: 3.4 GB, of which HBM
-// takes 3.9 GB a ms (0.98 ms).  Rows that are no multiples of 16 bytes: the warps' copies (2203200 x 256 -> 372 0.80 ms, -> 384 0.56).
+// takes 3.9 GB a ms (0.98 ms).  Rows that are no multiples of 16 bytes: the warps' copies (2203200 x 256 -> 372 0.71 ms, -> 384 0.53).
 //
 // Roles (640 threads): warp 0 copies, warp 1 issues the products, warp 2 has the TMEM, warps 4-19 the epilogue; weight gradient: warps 2 and 3 the
 // sums of d_z.

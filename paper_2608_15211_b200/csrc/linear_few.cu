@@ -1,8 +1,8 @@
 // The forward product for a few rows (a conditioning vector, a single token): y = act(x w' + bias) + residual for up to 8 rows of x, on the
 // plain arithmetic units, 16-bit or e4m3 operands.  Every weight is read once, in runs of 512 bytes a warp, and meets all rows of x in fp32.
 // A block takes kOut rows of w for each of its groups of warps, the warps of a group share the sum over k; no operand needs padding.
-// What bounds it: HBM (2 x 4096 -> 8192 reads 67 MB).  The tensor-core kernel spends its tiles of 128 rows on zeros there: it
-// keeps a tenth of the bytes in flight that this one does.
+// What bounds it: HBM behind a launch's latency (weights not in L2: 2 x 4096 -> 8192, 67 MB, 17.8 us; 2 x 8192 -> 8192, 134 MB, 30.6 us).  The
+// tensor-core kernel spends its tiles of 128 rows on zeros there: it keeps a tenth of the bytes in flight that this one does.
 #include <cuda_fp8.h>
 
 #include "block_act.cuh"
