@@ -18,7 +18,7 @@
 // What bounds it: the tensor pipe where the sum is long (156672 x 4096 -> 4096 3.35 ms, 1569 TFLOP/s, the pipe busy in 91 % of the cycles; e4m3 to 16384 with
 // GELU 7.2 ms, 2930 TFLOP/s), over seconds the power cap (4.1 and 9.0 ms); the epilogue where it is short (550800 x 384 -> 1536 with GELU 0.85 ms, two
 // reciprocals or exponentials an output in a unit that takes 16 a clock and SM, busy in half the cycles), with z besides the writes: 3.4 GB, of which HBM
-// takes 3.9 GB a ms (0.98 ms).  Rows that are no multiples of 16 bytes: the warps' copies (2203200 x 256 -> 372 0.71 ms, -> 384 0.53).
+// takes 3.9 GB a ms (0.98 ms).  Rows that are no multiples of 16 bytes: the warps' copies (2203200 x 256 -> 372 0.64 ms, -> 384 0.56).
 //
 // Roles (640 threads): warp 0 copies, warp 1 issues the products, warp 2 has the TMEM, warps 4-19 the epilogue; weight gradient: warps 2 and 3 the
 // sums of d_z.
@@ -228,36 +228,55 @@ __device__ __forceinline__ void sts(uint32_t at, uint32_t v) { asm volatile("st.
 __device__ __forceinline__ void sts(uint32_t at, uint16_t v) { asm volatile("st.shared.b16 [%0], %1;\n" ::"r"(at), "h"(v) : "memory"); }
 
 // A warp's tile <-> `rows` rows of global memory from g on (its first row and column; rows of `stride` elements), the first `cols` columns, in units
-// of T: for rows that are no multiples of 16 bytes.  Eight rows (of 8-byte units sixteen) are read before they are written.
-template <bool OUT, typename T>
-__device__ __forceinline__ void copy_tile_units(uint32_t tile, bool narrow, uint16_t* g, long long stride, int rows, int cols, int lane) {
-    constexpr int kUnit = sizeof(T) / 2, kAcross = 64 / kUnit, kLanes = kAcross < 32 ? kAcross : 32, kDown = 32 / kLanes;
+// of T: for rows that are no multiples of 16 bytes.  Eight rows (of 8-byte units sixteen) are read before they are written; their exchanged places
+// differ by constants, so that a unit costs a read, a write and a step of the address (2203200 x 256 -> 372 707 -> 638 us).
+template <bool OUT, bool NARROW, typename T>
+__device__ __forceinline__ void copy_tile_units(uint32_t tile, uint16_t* g, long long stride, int rows, int cols, int lane) {
+    constexpr int kUnit = sizeof(T) / 2, kAcross = 64 / kUnit, kLanes = kAcross < 32 ? kAcross : 32, kDown = 32 / kLanes, kPitch = NARROW ? 64 : 128;
     const int sub = lane / kLanes;
+    const long long step = kDown * stride * 2;
 #pragma unroll 1
     for (int col = (lane % kLanes) * kUnit; col < cols; col += kLanes * kUnit) {
-        uint16_t* p = g + sub * stride + col;
-        const uint32_t in_place = (col & 7) * 2;
+        char* p = (char*)(g + sub * stride + col);
+        uint32_t at = tile + place(sub, col >> 3, NARROW) + (col & 7) * 2;
 #pragma unroll 1
-        for (int r = sub; r < rows; r += 8 * kDown, p += 8 * kDown * stride) {
+        for (int left = rows - sub; left > 0; left -= 8 * kDown, at += 8 * kDown * kPitch) {
             T v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+            char* q = p;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (OUT) lds(tile + place(r + i * kDown, col >> 3, narrow) + in_place, v[i]);
-                else if (r + i * kDown < rows) v[i] = *reinterpret_cast<const T*>(p + i * kDown * stride);
+            for (int i = 0; i < 8; ++i) {              // (sub is 0, or 1 where kDown is 2: the row's number is sub ^ kDown i as well)
+                const uint32_t here = (at ^ place(kDown * i, 0, NARROW) % kPitch) + kDown * i * kPitch;
+                if (OUT) {
+                    lds(here, v[i]);
+                } else {
+                    if (kDown * i < left) v[i] = *reinterpret_cast<const T*>(q);
+                    q += step;
+                }
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                if (!OUT) sts(tile + place(r + i * kDown, col >> 3, narrow) + in_place, v[i]);
-                else if (r + i * kDown < rows) *reinterpret_cast<T*>(p + i * kDown * stride) = v[i];
+                const uint32_t here = (at ^ place(kDown * i, 0, NARROW) % kPitch) + kDown * i * kPitch;
+                if (!OUT) {
+                    sts(here, v[i]);
+                } else {
+                    if (kDown * i < left) *reinterpret_cast<T*>(q) = v[i];
+                    q += step;
+                }
             }
+            p = q;
         }
     }
 }
+template <bool OUT, bool NARROW>
+__device__ __forceinline__ void copy_tile(uint32_t tile, uint16_t* g, long long stride, int rows, int cols, int lane) {
+    if (((stride | cols) & 3) == 0) copy_tile_units<OUT, NARROW, unsigned long long>(tile, g, stride, rows, cols, lane);
+    else if (((stride | cols) & 1) == 0) copy_tile_units<OUT, NARROW, uint32_t>(tile, g, stride, rows, cols, lane);
+    else copy_tile_units<OUT, NARROW, uint16_t>(tile, g, stride, rows, cols, lane);
+}
 template <bool OUT>
 __device__ __forceinline__ void copy_tile(uint32_t tile, bool narrow, uint16_t* g, long long stride, int rows, int cols, int lane) {
-    if (((stride | cols) & 3) == 0) copy_tile_units<OUT, unsigned long long>(tile, narrow, g, stride, rows, cols, lane);
-    else if (((stride | cols) & 1) == 0) copy_tile_units<OUT, uint32_t>(tile, narrow, g, stride, rows, cols, lane);
-    else copy_tile_units<OUT, uint16_t>(tile, narrow, g, stride, rows, cols, lane);
+    if (narrow) copy_tile<OUT, true>(tile, g, stride, rows, cols, lane);
+    else copy_tile<OUT, false>(tile, g, stride, rows, cols, lane);
 }
 
 // 32 columns of a thread's row: out of TMEM (`acc`), through the epilogue, into the warp's tile from its 16-byte place `first` on.
@@ -700,7 +719,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_consta
                             if (own > at0) {
                                 const long long where = row0 * job.N + col + at0;
                                 copy_tile<true>(to, width == 32, (uint16_t*)job.e.y + where, job.N, rows, min(width, own - at0), lane);
-                                if (has_z) copy_tile<true>(to + kTile / 2, true, (uint16_t*)job.e.z + where, job.N, rows, min(width, own - at0), lane);
+                                if (has_z) copy_tile<true, true>(to + kTile / 2, (uint16_t*)job.e.z + where, job.N, rows, min(width, own - at0), lane);
                             }
                             __syncwarp();
                         }
