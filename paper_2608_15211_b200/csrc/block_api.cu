@@ -68,9 +68,8 @@ struct LinearLayout {
     size_t bytes;
 };
 
-// Few rows on the plain arithmetic units / on the tensor cores, us, operands in L2: 1 x 4096 -> 4096 4.9 / 12.4, 2 x 4096 -> 8192 10.2 / 20.3, 4 rows 16.4 / 20.5, 8 rows
-// 30.2 / 20.7, but 8 x 1024 -> 1024 3.2 / 8.5: a launch and a tile's latency against an arithmetic that grows with the rows.
-bool few_rows(const terra_linear_desc* d) { return d->rows <= 4 || (d->rows <= kFewRows && (long long)d->n_in * d->n_out <= 12000000); }
+// (the kernel for few rows / the tiles of 128 rows, us, weights not in L2: 8 x 8192 -> 8192 26.5 / 33.1, 8 x 4096 -> 8192 15.9 / 19.0, 8 x 1024 -> 1024 4.3 / 7.6)
+bool few_rows(const terra_linear_desc* d) { return d->rows <= kFewRows; }
 
 LinearLayout layout_linear(const terra_linear_desc* d, int call) {
     LinearLayout l = {};

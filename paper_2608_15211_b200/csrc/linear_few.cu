@@ -1,8 +1,11 @@
-// The forward product for a few rows (a conditioning vector, a single token): y = act(x w' + bias) + residual for up to 8 rows of x, on the
-// plain arithmetic units, 16-bit or e4m3 operands.  Every weight is read once, in runs of 512 bytes a warp, and meets all rows of x in fp32.
-// A block takes kOut rows of w for each of its groups of warps, the warps of a group share the sum over k; no operand needs padding.
-// What bounds it: HBM behind a launch's latency (weights not in L2: 2 x 4096 -> 8192, 67 MB, 17.8 us; 2 x 8192 -> 8192, 134 MB, 30.6 us).  The
-// tensor-core kernel spends its tiles of 128 rows on zeros there: it keeps a tenth of the bytes in flight that this one does.
+// The forward product for up to 8 rows of x (a conditioning vector, a single token): y = act(x w' + bias) + residual, 16-bit or e4m3 operands (those
+// made fp16, which is exact), on the warps' matrix instructions of 16 rows of w x 8 rows of x, sums in fp32.  Every weight is read once,
+// straight into the registers of its product: a lane takes 16 consecutive bytes of a row of w and of x for what the instruction calls columns
+// 2t, 2t + 1, 2t + 8, 2t + 9 and so on, which only changes the order of the sum.  The warps of a group share the sum over k; no operand needs padding.
+// What bounds it: HBM behind a launch's latency (weights not in L2: 2 x 4096 -> 8192, 67 MB, 15.1 us; 2 x 8192 -> 8192, 134 MB, 25.6 us; 8 rows 15.9 and
+// 26.5; e4m3 11.2 and 20.1).  tcgen05 wants 128 rows and its operands in shared memory, one more step between HBM and the product (16 rows 19.0 and 33.1
+// us).  On the plain arithmetic units, two conversions for a pair of weights and a multiplication for each row of x, these took 18.1 and 32.4 us with 2
+// rows, 23.5 and 33 with 8; one row, 8192 -> 8192, took 24.3 there and 25.5 here.
 #include <cuda_fp8.h>
 
 #include "block_act.cuh"
@@ -15,122 +18,124 @@
 namespace terra {
 namespace {
 
-constexpr int kWarps = 8;
+constexpr int kWarps = 16, kRows = 16, kDeep = 4;        // of a block; of w at a time; runs of k under way in a warp
 
-// V values of an operand's row in memory, as pairs of fp32 (V 1: the second is 0)
-template <bool E4M3, int V> struct Run;
-template <int V> struct Run<false, V> {
-    static constexpr int kPairs = V > 1 ? V / 2 : 1;
-    uint32_t w[kPairs];
-    __device__ __forceinline__ void load(const void* row, long long k) {
-        const uint16_t* p = (const uint16_t*)row + k;
-        if (V == 8) *reinterpret_cast<uint4*>(w) = __ldg(reinterpret_cast<const uint4*>(p));
-        else if (V == 2) w[0] = __ldg(reinterpret_cast<const uint32_t*>(p));
-        else w[0] = __ldg(p);
+// 16 bytes of an operand's row, the part of them that lies before the row's end; V: bytes that all rows are aligned to
+template <int V>
+__device__ __forceinline__ void load16(const char* row, int at, int bytes, uint32_t (&v)[4]) {
+    if (V == 16) {
+        uint4 u = make_uint4(0, 0, 0, 0);
+        if (at < bytes) u = __ldg(reinterpret_cast<const uint4*>(row + at));
+        v[0] = u.x; v[1] = u.y; v[2] = u.z; v[3] = u.w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[i] = 0;
+#pragma unroll
+            for (int j = 0; j < 4; j += V) {
+                const int a = at + 4 * i + j;
+                if (a < bytes) {
+                    const uint32_t u = V == 4 ? __ldg(reinterpret_cast<const uint32_t*>(row + a))
+                                     : V == 2 ? __ldg(reinterpret_cast<const uint16_t*>(row + a)) : __ldg(reinterpret_cast<const uint8_t*>(row + a));
+                    v[i] |= u << (8 * j);
+                }
+            }
+        }
     }
-    __device__ __forceinline__ Pair pair(int i) const { const float2 t = elem2_to_float2(w[i]); return pair_of(t.x, t.y); }
-};
-template <int V> struct Run<true, V> {
-    static constexpr int kPairs = V > 1 ? V / 2 : 1;
-    uint32_t w[V >= 4 ? V / 4 : 1];
-    __device__ __forceinline__ void load(const void* row, long long k) {
-        const uint8_t* p = (const uint8_t*)row + k;
-        if (V == 16) *reinterpret_cast<uint4*>(w) = __ldg(reinterpret_cast<const uint4*>(p));
-        else if (V == 4) w[0] = __ldg(reinterpret_cast<const uint32_t*>(p));
-        else w[0] = __ldg(p);
-    }
-    __device__ __forceinline__ Pair pair(int i) const {
-        const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[i >> 1] >> (16 * (i & 1))), __NV_E4M3);
-        const float2 t = __half22float2(*reinterpret_cast<const __half2*>(&h));
-        return pair_of(t.x, t.y);
-    }
-};
+}
 
-template <bool E4M3, int R, int V>
-__global__ void __launch_bounds__(32 * kWarps) linear_few_kernel(const LinearEpilogue e, const void* __restrict__ x, const void* __restrict__ w, int rows, int n_in, int n_out,
-                                                                 int share) {
-    constexpr int kOut = R == 8 ? 2 : 4, kValues = kOut * R, kElem = E4M3 ? 1 : 2;
-    __shared__ float sums[kWarps][kValues];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = warp % share, group = warp / share;
-    const int n0 = (blockIdx.x * (kWarps / share) + group) * kOut;
-    const char *xr[R], *wr[kOut];
-#pragma unroll
-    for (int r = 0; r < R; ++r) xr[r] = (const char*)x + (long long)min(r, rows - 1) * n_in * kElem;
-#pragma unroll
-    for (int o = 0; o < kOut; ++o) wr[o] = (const char*)w + (long long)min(n0 + o, n_out - 1) * n_in * kElem;
-    Pair acc[kOut][R];
-#pragma unroll
-    for (int o = 0; o < kOut; ++o)
-#pragma unroll
-        for (int r = 0; r < R; ++r) acc[o][r] = 0;
+template <bool E4M3>
+__device__ __forceinline__ void multiply(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+#ifdef TERRA_ELEM_F16
+    constexpr bool kHalf = true;
+#else
+    constexpr bool kHalf = E4M3;
+#endif
+    if (kHalf)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};\n"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};\n"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t half2_of_e4m3(uint32_t two) {
+    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two, __NV_E4M3);
+    return (uint32_t)h.x | (uint32_t)h.y << 16;
+}
+
+// A group of `share` warps has `height` rows of w, from n0 on: 4, 8 or kRows.
+template <bool E4M3, int V>
+__global__ void __launch_bounds__(32 * kWarps, 2) linear_few_kernel(const LinearEpilogue e, const char* __restrict__ x, const char* __restrict__ w, int rows, int n_in,
+                                                                    int n_out, int share, int height) {
+    __shared__ float sums[kWarps][8][kRows];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = warp % share, group = warp / share, groups = kWarps / share;
+    const int g = lane >> 2, t = lane & 3, bytes = n_in * (E4M3 ? 1 : 2), n0 = (blockIdx.x * groups + group) * height;
+    const char* w0 = w + (long long)min(n0 + g, n_out - 1) * bytes;
+    const char* w1 = w + (long long)min(n0 + 8 + g, n_out - 1) * bytes;
+    const char* xr = x + (long long)g * bytes;
+    const int x_bytes = g < rows ? bytes : 0, w0_bytes = g < height ? bytes : 0, w1_bytes = height > 8 ? bytes : 0;        // rows that are not there are zeros
+    float c[4] = {0.f, 0.f, 0.f, 0.f};
     let_dependents_start();
     wait_for_prerequisites();
-#pragma unroll (R >= 4 ? 2 : 4)
-    for (int k = (part * 32 + lane) * V; k < n_in; k += share * 32 * V) {
-        Run<E4M3, V> wv[kOut], xv[R];
+#pragma unroll 1
+    for (int at = part * 64 + t * 16; at - t * 16 < bytes && n0 < n_out; at += kDeep * share * 64) {
+        uint32_t a[kDeep][4], b[kDeep][4];
 #pragma unroll
-        for (int o = 0; o < kOut; ++o) wv[o].load(wr[o], k);
+        for (int i = 0; i < kDeep; ++i) {
+            load16<V>(w0, at + i * share * 64, w0_bytes, a[i]);
+            load16<V>(w1, at + i * share * 64, w1_bytes, b[i]);
+        }
 #pragma unroll
-        for (int r = 0; r < R; ++r) xv[r].load(xr[r], k);
+        for (int i = 0; i < kDeep; ++i) {
+            uint32_t xv[4];
+            load16<V>(xr, at + i * share * 64, x_bytes, xv);
 #pragma unroll
-        for (int i = 0; i < Run<E4M3, V>::kPairs; ++i) {
-            Pair xp[R];
-#pragma unroll
-            for (int r = 0; r < R; ++r) xp[r] = xv[r].pair(i);
-#pragma unroll
-            for (int o = 0; o < kOut; ++o) {
-                const Pair wp = wv[o].pair(i);
-#pragma unroll
-                for (int r = 0; r < R; ++r) acc[o][r] = pfma(wp, xp[r], acc[o][r]);
+            for (int s = 0; s < 2; ++s) {
+                const uint32_t p = a[i][2 * s], q = a[i][2 * s + 1], u = b[i][2 * s], v = b[i][2 * s + 1], m = xv[2 * s], n = xv[2 * s + 1];
+                if (E4M3) {
+                    multiply<true>(c, half2_of_e4m3(p & 0xffff), half2_of_e4m3(u & 0xffff), half2_of_e4m3(p >> 16), half2_of_e4m3(u >> 16), half2_of_e4m3(m & 0xffff), half2_of_e4m3(m >> 16));
+                    multiply<true>(c, half2_of_e4m3(q & 0xffff), half2_of_e4m3(v & 0xffff), half2_of_e4m3(q >> 16), half2_of_e4m3(v >> 16), half2_of_e4m3(n & 0xffff), half2_of_e4m3(n >> 16));
+                } else {
+                    multiply<false>(c, p, u, q, v, m, n);
+                }
             }
         }
     }
 #pragma unroll
-    for (int o = 0; o < kOut; ++o)
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            float a, b;
-            split_pair(acc[o][r], a, b);
-            a += b;
-#pragma unroll
-            for (int d = 16; d > 0; d >>= 1) a += __shfl_xor_sync(0xffffffffu, a, d);
-            if (lane == 0) sums[warp][r * kOut + o] = a;
-        }
+    for (int i = 0; i < 4; ++i) sums[warp][2 * t + (i & 1)][g + 8 * (i >> 1)] = c[i];
     __syncthreads();
-    // a thread of each group to an output
-    const int out_group = threadIdx.x / kValues, v = threadIdx.x % kValues, r = v / kOut, n = (blockIdx.x * (kWarps / share) + out_group) * kOut + v % kOut;
-    if (out_group >= kWarps / share || r >= rows || n >= n_out) return;
-    float z = 0.f;
-    for (int i = 0; i < share; ++i) z += sums[out_group * share + i][v];
-    const long long at = (long long)r * n_out + n;
-    if (E4M3) z = z * e.x_scale[r] * e.w_scale[n];
-    if (e.bias) z += e.bias[n];
-    if (e.z) ((uint16_t*)e.z)[at] = (uint16_t)pack_elem(z, 0.f);
-    const float res = e.residual ? elem2_to_float2(((const uint16_t*)e.residual)[at]).x : 0.f;
-    with_act(e.activation, [&](auto tag) { ((uint16_t*)e.y)[at] = (uint16_t)pack_elem(act<decltype(tag)::value>(z) + res, 0.f); });
-}
-
-template <bool E4M3, int R>
-auto kernel_for(int n_in) {
-    constexpr int kWide = E4M3 ? 16 : 8, kMid = E4M3 ? 4 : 2;
-    return n_in % kWide == 0 ? linear_few_kernel<E4M3, R, kWide> : n_in % kMid == 0 ? linear_few_kernel<E4M3, R, kMid> : linear_few_kernel<E4M3, R, 1>;
+    // a thread to an output
+    for (int i = threadIdx.x; i < groups * rows * height; i += 32 * kWarps) {
+        const int o = i % height, r = i / height % rows, of = i / height / rows, n = (blockIdx.x * groups + of) * height + o;
+        if (n >= n_out) continue;
+        float z = 0.f;
+        for (int s = 0; s < share; ++s) z += sums[of * share + s][r][o];
+        const long long at = (long long)r * n_out + n;
+        if (E4M3) z = z * e.x_scale[r] * e.w_scale[n];
+        if (e.bias) z += e.bias[n];
+        if (e.z) ((uint16_t*)e.z)[at] = (uint16_t)pack_elem(z, 0.f);
+        const float res = e.residual ? elem2_to_float2(((const uint16_t*)e.residual)[at]).x : 0.f;
+        with_act(e.activation, [&](auto tag) { ((uint16_t*)e.y)[at] = (uint16_t)pack_elem(act<decltype(tag)::value>(z) + res, 0.f); });
+    }
 }
 
 }  // namespace
 
 cudaError_t launch_linear_few(bool e4m3, int rows, int n_in, int n_out, const void* x, const void* w, const LinearEpilogue& epi, cudaStream_t stream) {
-    const int R = rows <= 1 ? 1 : rows <= 2 ? 2 : rows <= 4 ? 4 : 8, out = R == 8 ? 2 : 4;
-    const int wide = e4m3 ? 16 : 8, mid = e4m3 ? 4 : 2, v = n_in % wide == 0 ? wide : n_in % mid == 0 ? mid : 1;
-    // warps that share a sum: as many as fit the device at a time (24 an SM, for one row 40), so that each has many runs and none waits for a place
-    // (4096 -> 8192: 2 rows with one warp to a sum 17.1 us, with two 18.6; 8192 -> 8192: 1 row with one warp 29.5, with two 24.2)
-    const int sums = (n_out + out - 1) / out;
-    int share = 1;
-    while (share < kWarps && share * 32 * v < n_in && 2ll * sums * share <= (R == 1 ? 40ll : 24ll) * kPlanSms) share *= 2;
-    const int per_block = kWarps / share * out;
-    auto kern = e4m3 ? (R == 1 ? kernel_for<true, 1>(n_in) : R == 2 ? kernel_for<true, 2>(n_in) : R == 4 ? kernel_for<true, 4>(n_in) : kernel_for<true, 8>(n_in))
-                     : (R == 1 ? kernel_for<false, 1>(n_in) : R == 2 ? kernel_for<false, 2>(n_in) : R == 4 ? kernel_for<false, 4>(n_in) : kernel_for<false, 8>(n_in));
+    const int bytes = n_in * (e4m3 ? 1 : 2), runs = (bytes + 63) / 64;
+    constexpr long long kFit = 2 * kWarps * kPlanSms;        // warps on the GPU at a time
+    // Rows of w at a time: fewer where that gives more SMs something to read (3 x 4096 -> 372 5.7 -> 5.2 us, 1 x 16384 -> 64 13.1 -> 12.0).
+    int height = kRows, share = 1;
+    while (height > 4 && 2ll * ((n_out + height - 1) / height) * (runs < kWarps ? runs : kWarps) <= kFit) height /= 2;
+    // Warps that share a sum: as many as have 2 kDeep runs each, and more, down to one run, while all of them are on the GPU at a time.  (With kDeep runs each
+    // 1 x 1024 -> 65536 29.7 us, with 2 kDeep 28.0; no more warps than are on the GPU at a time: 2 x 8192 -> 8192 28.7 us against 25.6.)
+    const int tiles = (n_out + height - 1) / height;
+    while (share < kWarps && (4 * share * kDeep <= runs || (2 * share <= runs && 2ll * tiles * share <= kFit))) share *= 2;
+    const int groups = kWarps / share;
+    auto kern = e4m3 ? (bytes % 16 == 0 ? linear_few_kernel<true, 16> : bytes % 4 == 0 ? linear_few_kernel<true, 4> : linear_few_kernel<true, 1>)
+                     : (bytes % 16 == 0 ? linear_few_kernel<false, 16> : bytes % 4 == 0 ? linear_few_kernel<false, 4> : linear_few_kernel<false, 2>);
     prof_begin("linear_few_kernel", stream);
-    const cudaError_t e = launch_dependent(kern, (unsigned)((n_out + per_block - 1) / per_block), 32u * kWarps, 0, stream, epi, x, w, rows, n_in, n_out, share);
+    const cudaError_t e = launch_dependent(kern, (unsigned)((tiles + groups - 1) / groups), 32u * kWarps, 0, stream, epi, (const char*)x, (const char*)w, rows, n_in, n_out, share, height);
     count_launch(stream);
     return e;
 }

@@ -155,3 +155,33 @@ def test_an_activation_alone(n):
     assert (mem[:8] == -7).all() and (mem[8 + n:] == -7).all()
     terra.terra_activation_bwd(z, dy, "silu", d_z=dy)       # over the gradient
     assert torch.equal(dy, d_z)
+
+
+@pytest.mark.parametrize("e4m3", [False, True], ids=["16", "e4m3"])
+@pytest.mark.parametrize("rows,n_in,n_out", [(1, 16384, 64), (3, 4096, 372), (6, 1000, 5001), (2, 40, 65536), (4, 4094, 300), (5, 4095, 257), (8, 1, 1), (7, 2052, 17), (8, 8192, 1030)])
+def test_few_rows_are_exact_and_do_not_meet(rows, n_in, n_out, e4m3):
+    g = gen("few", rows, n_in, e4m3)
+    x, w, r = ints(g, rows, n_in), ints(g, n_out, n_in), ints(g, rows, n_out, dtype=F16)
+    b = torch.randint(-4, 5, (n_out,), generator=g, device="cuda").float()
+    mem = torch.full((rows * n_out + 16,), -7.0, device="cuda", dtype=F16)
+    y = mem[8:8 + rows * n_out].view(rows, n_out)
+
+    def call(x, r):
+        if not e4m3:
+            return terra.terra_linear_fwd(x.to(F16), w.to(F16), bias=b, residual=r, activation="relu", y=y)[0]
+        xs = torch.full((rows,), 2.0, device="cuda")
+        return terra.terra_linear_fwd_e4m3((x / 2).to(E4M3), xs, w.to(E4M3), torch.ones(n_out, device="cuda"), bias=b, residual=r, activation="relu", dtype=F16, y=y)
+
+    # whole numbers (halves, in 8 bits): the sums are exact, only the last rounding is left
+    ref = torch.relu(x.double() @ w.double().t() + b.double()) + r.double()
+    held("y", call(x, r), ref, 0, F16)
+    assert (mem[:8] == -7).all() and (mem[8 + rows * n_out:] == -7).all()
+    first = y.clone()
+    if rows > 1:                                       # a row of NaN stays with itself
+        bad = x.clone()
+        bad[-1] = float("nan")
+        call(bad, r)
+        assert torch.equal(y[:-1], first[:-1]) and y[-1].isnan().all()
+    w[-1] = float("nan")                               # and an output's weights with that output
+    call(x, r)
+    assert torch.equal(y[:, :-1], first[:, :-1]) and y[:, -1].isnan().all()
