@@ -11,9 +11,11 @@
 // The epilogue works on a warp's 32 rows x 64 columns at a time, a row to a thread, two columns to an instruction; the residual comes and the
 // results go as tiles in shared memory that the copy engine moves (rows that are no multiples of 16 bytes: the warp itself, in whole rows).
 //
-// The tensor cores' sum over k is not rounded to nearest, and its error grows with the number of steps.  The weight gradient, a sum over all
-// rows that comes out in fp32, therefore leaves TMEM every kLinearChunk stages and is added up in registers (156672 rows of N(0, 1) in fp16: 3.6e-7 off in
-// the 2-norm, with 16 stages 1.2e-6, at the same time).
+// The tensor cores' sum over k is cut off, not rounded to nearest, and its error grows with the number of steps, four a stage: 1.9e-8 of the 2-norm a step
+// on N(0, 1), 1.05e-7 where all terms have one sign.  The weight gradient, a sum over all rows that comes out in fp32, therefore leaves TMEM every kLinearChunk
+// stages and is added up in registers (156672 rows of N(0, 1) in fp16: 3.6e-7 off in the 2-norm, with 16 stages 1.2e-6, at the same time).  The other products,
+// whose results are rounded to 16 bits, leave it every kLinearLongChunk stages: terms of one sign are then 2.6e-5 off at most, a nineteenth of fp16's half
+// step.  (65536 features in one go: 4.3e-4.  Every 32 stages 4096 -> 4096 takes 3 % longer for half of the error, every 16 another 1 %, e4m3 with GELU 13 %.)
 //
 // What bounds it: the tensor pipe where the sum is long (156672 x 4096 -> 4096 3.35 ms, 1569 TFLOP/s, the pipe busy in 91 % of the cycles; e4m3 to 16384 with
 // GELU 7.2 ms, 2930 TFLOP/s), over seconds the power cap (4.1 and 9.0 ms); the epilogue where it is short (550800 x 384 -> 1536 with GELU 0.85 ms, two
@@ -345,8 +347,13 @@ __device__ __forceinline__ void write_sums(uint32_t tile, float* out, long long 
 
 // MAP: the rows of the outputs (and of the residual or z_in) are multiples of 16 bytes and the copy engine moves them; else the warps do.  (One kernel with
 // both spilled registers around the warps' copies: 2203200 x 256 -> 384 558 -> 1032 us.)
-template <bool PAIR, int KIND, bool E4M3, bool MAP, int TILES>
+// LONG: the sum leaves TMEM every kLinearLongChunk stages, for sums that have more.  (An instantiation of its own: the 64 sums that a thread holds spill
+// registers around the epilogue.)
+template <bool PAIR, int KIND, bool E4M3, bool MAP, int TILES, bool LONG>
 __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Job job) {
+    static_assert(!LONG || TILES == 1, "two tiles a warp are for short sums");
+    constexpr bool kInChunks = LONG || KIND == kLinearWeights;
+    constexpr int kChunk = KIND == kLinearWeights ? kLinearChunk : kLinearLongChunk;
     constexpr int CTAS = PAIR ? 2 : 1;
     constexpr int kStages = Stages<TILES>::value, kOffTiles = kStages * 2 * kOperand;
     constexpr int kTileRows = 128 * CTAS;
@@ -443,7 +450,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_consta
             for (; at.there() && ok; at.next()) {
                 const int k1 = at.k1();
                 for (int kb = at.k0(); kb < k1 && ok;) {
-                    const int end = KIND == kLinearWeights ? min(k1, kb + kLinearChunk) : k1;
+                    const int end = kInChunks ? min(k1, kb + kChunk) : k1;
                     const uint32_t buf = done & 1, acc = tmem + buf * kAccCols;
                     ok = wait_asleep(bar(kBAccEmpty + buf), ((done >> 1) & 1) ^ 1u, cta_abort);
                     if (!ok) break;
@@ -538,31 +545,36 @@ __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_consta
             __syncwarp();
             if (lane == 0) arrive_leader<PAIR>(bar(kBAccEmpty + buf));
         };
-        if constexpr (KIND == kLinearWeights) {
+        // a unit's sum over all of its chunks along k, this warp's 64 columns from col0 on (none: the warp only keeps in step)
+        auto add_up = [&](float (&acc)[64], int col0, bool some) {
+            const int k1 = at.k1();
+#pragma unroll
+            for (int i = 0; i < 64; ++i) acc[i] = 0.f;
+            for (int kb = at.k0(); kb < k1; kb += kChunk, ++done) {
+                const uint32_t buf = done & 1;
+                ok = wait_asleep(bar(kBAccFull + buf), (done >> 1) & 1, cta_abort);
+                if (!ok) break;
+                tc_fence_after();
+                if (some)
+#pragma unroll
+                    for (int p = 0; p < 4; ++p)
+                        if (col0 + 16 * p < job.bn) {
+                            uint32_t t[16];
+                            tmem_ld16(lane_tmem + buf * kAccCols + col0 + 16 * p, t);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) acc[16 * p + i] += __uint_as_float(t[i]);
+                        }
+                give_back(buf);
+            }
+        };
+        if (kInChunks && (KIND == kLinearWeights || job.e.sums)) {
             for (; at.there() && ok; at.next(), next_chunk()) {
                 const long long row0 = at.m0(kTileRows) + 128 * rank + 32 * quarter;
-                const int n0 = at.n0(), k1 = at.k1();
+                const int n0 = at.n0();
                 const int chunk = first_chunk, col0 = 64 * chunk;          // (as many groups as chunks: a group has one at most)
                 float acc[64];
-#pragma unroll
-                for (int i = 0; i < 64; ++i) acc[i] = 0.f;
-                for (int kb = at.k0(); kb < k1 && ok; kb += kLinearChunk, ++done) {
-                    const uint32_t buf = done & 1;
-                    ok = wait_asleep(bar(kBAccFull + buf), (done >> 1) & 1, cta_abort);
-                    if (!ok) break;
-                    tc_fence_after();
-                    if (chunk < chunks)
-#pragma unroll
-                        for (int p = 0; p < 4; ++p)
-                            if (col0 + 16 * p < job.bn) {
-                                uint32_t t[16];
-                                tmem_ld16(lane_tmem + buf * kAccCols + col0 + 16 * p, t);
-                                tmem_ld_wait();
-#pragma unroll
-                                for (int i = 0; i < 16; ++i) acc[16 * p + i] += __uint_as_float(t[i]);
-                            }
-                    give_back(buf);
-                }
+                add_up(acc, col0, chunk < chunks);
                 if (!ok || chunk >= chunks) continue;
                 float* sums = job.e.sums + (size_t)at.at.split * job.M * job.N;
 #pragma unroll
@@ -575,7 +587,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_consta
                         __syncwarp();
                     }
             }
-        } else if (job.e.sums) {
+        } else if (!kInChunks && job.e.sums) {
             for (; at.there() && ok; at.next(), ++done) {        // parts of a split sum
                 const long long row0 = at.m0(kTileRows) + 128 * rank + 32 * quarter;
                 const int n0 = at.n0();
@@ -604,7 +616,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_consta
                 give_back(buf);
                 next_chunk();
             }
-        } else {
+        } else if constexpr (KIND != kLinearWeights) {
             // A tile takes the residual (or z_in) first and y over it, each thread its row.  One tile: with z a chunk goes in two pieces of 32 columns, y in
             // the first 2 KB of the tile and z in the others.  Two tiles: z has the second, or else the chunks take them in turn, and the next chunk's
             // residual comes while this one is worked on.
@@ -629,10 +641,11 @@ __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_consta
             };
             // whether this group has a chunk of a unit
             auto has_chunk = [&](const Units& u, int chunk) { return chunk < chunks && u.n0() + 64 * chunk < job.N && u.m0(kTileRows) + 128 * rank + 32 * quarter < job.M; };
-            for (; at.there() && ok; at.next(), ++done) {
+            for (; at.there() && ok; at.next(), done += LONG ? 0 : 1) {
                 const long long row0 = at.m0(kTileRows) + 128 * rank + 32 * quarter;
                 const int n0 = at.n0();
                 const uint32_t buf = done & 1, acc = lane_tmem + buf * kAccCols;
+                float sum[LONG ? 64 : 1];
                 const int rows = (int)min(32ll, job.M - row0);
                 const uint32_t t = TILES == 2 && !has_z ? taken & 1 : 0, to = tile + t * kTile;
                 const bool mine = has_chunk(at, first_chunk);
@@ -645,7 +658,8 @@ __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_consta
                         if (E4M3) prefetch_l1(job.e.w_scale + c + 32 * lane);
                     }
                 }
-                ok = wait_asleep(bar(kBAccFull + buf), (done >> 1) & 1, cta_abort);
+                if constexpr (LONG) add_up(sum, 64 * first_chunk, mine);
+                else ok = wait_asleep(bar(kBAccFull + buf), (done >> 1) & 1, cta_abort);
                 if (!ok) {
                     if (mine && fetched && lane == 0) {        // it lands before this CTA ends
                         volatile int ignore = 0;
@@ -654,7 +668,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_consta
                     break;
                 }
                 tc_fence_after();
-                bool given = false;
+                bool given = LONG;
                 if (const int chunk = first_chunk; mine) {     // (as many groups as chunks: a group has one at most)
                     const int col0 = 64 * chunk, col = n0 + col0, cols = min(64, job.bn - col0), own = min(cols, job.N - col);
                     float x_scale = 1.f;
@@ -690,11 +704,19 @@ __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_consta
                             }
                         }
                         uint32_t cur[32];
-                        tmem_ld32(acc + col0 + p0, cur);
-                        tmem_ld_wait();
-                        if (p0 + 32 >= cols) {         // the accumulator has been read
-                            give_back(buf);
-                            given = true;
+                        if constexpr (LONG) {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) {
+                                cur[i] = __float_as_uint(sum[i]);
+                                sum[i] = sum[i + 32];  // the next 32 columns
+                            }
+                        } else {
+                            tmem_ld32(acc + col0 + p0, cur);
+                            tmem_ld_wait();
+                            if (p0 + 32 >= cols) {     // the accumulator has been read
+                                give_back(buf);
+                                given = true;
+                            }
                         }
                         with_act(job.e.activation, [&](auto tag) {
                             constexpr int ACT = decltype(tag)::value;
@@ -898,9 +920,9 @@ bool encode_map(CUtensorMap* map, const void* base, long long fast, long long sl
                CU_TENSOR_MAP_INTERLEAVE_NONE, box_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <bool PAIR, int KIND, bool E4M3, bool MAP, int TILES>
+template <bool PAIR, int KIND, bool E4M3, bool MAP, int TILES, bool LONG>
 cudaError_t launch_one(const Maps& maps, Job& job, int sm_count, cudaStream_t stream) {
-    auto kern = linear_kernel<PAIR, KIND, E4M3, MAP, TILES>;
+    auto kern = linear_kernel<PAIR, KIND, E4M3, MAP, TILES, LONG>;
     cudaError_t e = prepare_kernel((const void*)kern, kSmem);
     if (e != cudaSuccess) return e;
     const unsigned units = (unsigned)(job.groups * job.group * job.n_tiles * job.splits), fit = (unsigned)sm_count / (PAIR ? 2 : 1), at_a_time = units < fit ? units : fit;
@@ -928,12 +950,17 @@ cudaError_t launch_one(const Maps& maps, Job& job, int sm_count, cudaStream_t st
 // where a thread for four columns leaves most of the device idle and adds up more than a few parts
 bool splits_are_many(int splits, long long quads) { return splits >= 4 && quads <= 256ll * kPlanSms; }
 
+template <int KIND, bool E4M3, bool LONG>
+cudaError_t launch_one_tile(bool pair, bool map, const Maps& maps, Job& job, int sm_count, cudaStream_t stream) {
+    if (pair) return map ? launch_one<true, KIND, E4M3, true, 1, LONG>(maps, job, sm_count, stream) : launch_one<true, KIND, E4M3, false, 1, LONG>(maps, job, sm_count, stream);
+    return map ? launch_one<false, KIND, E4M3, true, 1, LONG>(maps, job, sm_count, stream) : launch_one<false, KIND, E4M3, false, 1, LONG>(maps, job, sm_count, stream);
+}
 template <int KIND, bool E4M3>
 cudaError_t launch_kind(bool pair, bool map, int tiles, const Maps& maps, Job& job, int sm_count, cudaStream_t stream) {
     if constexpr (!E4M3)
-        if (pair && tiles == 2) return launch_one<true, KIND, E4M3, true, 2>(maps, job, sm_count, stream);
-    if (pair) return map ? launch_one<true, KIND, E4M3, true, 1>(maps, job, sm_count, stream) : launch_one<true, KIND, E4M3, false, 1>(maps, job, sm_count, stream);
-    return map ? launch_one<false, KIND, E4M3, true, 1>(maps, job, sm_count, stream) : launch_one<false, KIND, E4M3, false, 1>(maps, job, sm_count, stream);
+        if (pair && tiles == 2) return launch_one<true, KIND, E4M3, true, 2, false>(maps, job, sm_count, stream);
+    return job.kb_per_split > kLinearLongChunk ? launch_one_tile<KIND, E4M3, true>(pair, map, maps, job, sm_count, stream)
+                                               : launch_one_tile<KIND, E4M3, false>(pair, map, maps, job, sm_count, stream);
 }
 
 }  // namespace
@@ -995,7 +1022,7 @@ cudaError_t launch_linear(int kind, bool e4m3, const LinearPlan& p, long long M,
     if (kind == kLinearForward && e4m3) e = launch_kind<kLinearForward, true>(p.pair, map, tiles, maps, job, sm_count, stream);
     else if (kind == kLinearForward) e = launch_kind<kLinearForward, false>(p.pair, map, tiles, maps, job, sm_count, stream);
     else if (kind == kLinearInput) e = launch_kind<kLinearInput, false>(p.pair, map, tiles, maps, job, sm_count, stream);
-    else e = p.pair ? launch_one<true, kLinearWeights, false, true, 1>(maps, job, sm_count, stream) : launch_one<false, kLinearWeights, false, true, 1>(maps, job, sm_count, stream);
+    else e = p.pair ? launch_one<true, kLinearWeights, false, true, 1, false>(maps, job, sm_count, stream) : launch_one<false, kLinearWeights, false, true, 1, false>(maps, job, sm_count, stream);
     if (e == cudaSuccess && p.splits == 1 && a_splits > 1) return launch_sum_partials(a_parts, a_splits, (int)M, epi.a_sums, stream);
     if (e != cudaSuccess || p.splits == 1) return e;
     const long long quads = M * ((N + 3) / 4);
