@@ -77,6 +77,9 @@ struct LinearPlan {
 };
 LinearPlan plan_linear(int kind, bool e4m3, long long M, int N, long long K);
 
+// What stands for 64 columns' bias where there is none: read as 16-byte vectors.
+struct alignas(16) NoBias { float values[64]; };
+
 struct LinearEpilogue {
     const float *bias, *x_scale, *w_scale;
     const void *residual, *z_in;

@@ -200,7 +200,7 @@ __device__ __forceinline__ uint32_t pack2(Pair p) { float a, b; split_pair(p, a,
 
 __device__ __forceinline__ void prefetch_l1(const float* p) { asm volatile("prefetch.global.L1 [%0];\n" ::"l"(p)); }
 
-__device__ float g_zeros[64];          // what stands for a bias that is not there
+__device__ NoBias g_no_bias;
 
 // p[col .. col + 15], the same for all threads of a warp; from the n-th value on some that is there
 __device__ __forceinline__ void row_values(const float* p, int col, int n, float (&v)[16]) {
@@ -289,7 +289,7 @@ __device__ __forceinline__ void finish32(const uint32_t (&acc)[32], const Linear
     for (int part = 0; part < 2; ++part) {
         float b[16], w[16];
         if (KIND == kLinearForward) {
-            row_values(e.bias ? e.bias : g_zeros, e.bias ? col + 16 * part : 0, e.bias ? n : 64, b);
+            row_values(e.bias ? e.bias : g_no_bias.values, e.bias ? col + 16 * part : 0, e.bias ? n : 64, b);
             if (E4M3) row_values(e.w_scale, col + 16 * part, n, w);
         }
 #pragma unroll
