@@ -202,17 +202,18 @@ __device__ __forceinline__ void prefetch_l1(const float* p) { asm volatile("pref
 
 __device__ NoBias g_no_bias;
 
-// p[col .. col + 15], the same for all threads of a warp; from the n-th value on some that is there
+// p[col .. col + 15], the same for all threads of a warp; from the n-th value on some that is there.  (Plain loads, here and wherever a kernel reads behind
+// wait_for_prerequisites(): the launch before may write these values while this kernel is already resident, so they are not read-only for its lifetime.)
 __device__ __forceinline__ void row_values(const float* p, int col, int n, float (&v)[16]) {
     if (col + 16 <= n) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const float4 t = __ldg(reinterpret_cast<const float4*>(p + col) + q);
+            const float4 t = reinterpret_cast<const float4*>(p + col)[q];
             v[4 * q] = t.x; v[4 * q + 1] = t.y; v[4 * q + 2] = t.z; v[4 * q + 3] = t.w;
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = __ldg(p + min(col + i, n - 1));
+        for (int i = 0; i < 16; ++i) v[i] = p[min(col + i, n - 1)];
     }
 }
 
@@ -672,7 +673,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_consta
                 if (const int chunk = first_chunk; mine) {     // (as many groups as chunks: a group has one at most)
                     const int col0 = 64 * chunk, col = n0 + col0, cols = min(64, job.bn - col0), own = min(cols, job.N - col);
                     float x_scale = 1.f;
-                    if (E4M3 && lane < rows) x_scale = __ldg(job.e.x_scale + row0 + lane);
+                    if (E4M3 && lane < rows) x_scale = job.e.x_scale[row0 + lane];
 #pragma unroll 1
                     for (int p0 = 0; p0 < cols; p0 += 32) {
                         if (p0 == 0 || width == 32) {          // a new tile
@@ -831,8 +832,8 @@ __device__ __forceinline__ void part4(const float* p, int col, int N, float (&v)
 
 // Joins the parts of a split product: the sum over the splits, in a fixed order, then the epilogue.
 template <int KIND>
-__global__ void __launch_bounds__(256) linear_join_kernel(const LinearEpilogue e, const float* __restrict__ parts, int splits, long long M, int N, float* out,
-                                                          const float* __restrict__ a_parts, int a_splits) {
+__global__ void __launch_bounds__(256) linear_join_kernel(const LinearEpilogue e, const float* parts, int splits, long long M, int N, float* out,
+                                                          const float* a_parts, int a_splits) {
     let_dependents_start();
     wait_for_prerequisites();
     const int per_row = (N + 3) / 4;
@@ -858,8 +859,8 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const LinearEpilogue e
 // The same for outputs too small to fill the device so: 8 threads share the parts of four columns.  (A thread that adds 64 parts up alone waits for
 // memory eight times.)  Blocks from `quads` on add up a_parts.
 template <int KIND>
-__global__ void __launch_bounds__(256) linear_join_small_kernel(const LinearEpilogue e, const float* __restrict__ parts, int splits, long long M, int N, float* out,
-                                                                const float* __restrict__ a_parts, int a_splits, int quads) {
+__global__ void __launch_bounds__(256) linear_join_small_kernel(const LinearEpilogue e, const float* parts, int splits, long long M, int N, float* out,
+                                                                const float* a_parts, int a_splits, int quads) {
     __shared__ float sums[8][32][4];
     let_dependents_start();
     wait_for_prerequisites();

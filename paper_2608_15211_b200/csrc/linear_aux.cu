@@ -60,7 +60,7 @@ __global__ void __launch_bounds__(1024) sum_partials_kernel(const float* partial
 #endif
 
 // 256 columns (32 threads x 8) and 8 rows at a time to a block; the row slice blockIdx.y of the partial sums
-__global__ void __launch_bounds__(kBlock) column_sums_kernel(const uint16_t* __restrict__ x, long long rows, int columns, long long stride, float* partial) {
+__global__ void __launch_bounds__(kBlock) column_sums_kernel(const uint16_t* x, long long rows, int columns, long long stride, float* partial) {
     __shared__ float sums[8][256];
     let_dependents_start();
     wait_for_prerequisites();

@@ -25,7 +25,7 @@ template <int V>
 __device__ __forceinline__ void load16(const char* row, int at, int bytes, uint32_t (&v)[4]) {
     if (V == 16) {
         uint4 u = make_uint4(0, 0, 0, 0);
-        if (at < bytes) u = __ldg(reinterpret_cast<const uint4*>(row + at));
+        if (at < bytes) u = *reinterpret_cast<const uint4*>(row + at);
         v[0] = u.x; v[1] = u.y; v[2] = u.z; v[3] = u.w;
     } else {
 #pragma unroll
@@ -35,8 +35,8 @@ __device__ __forceinline__ void load16(const char* row, int at, int bytes, uint3
             for (int j = 0; j < 4; j += V) {
                 const int a = at + 4 * i + j;
                 if (a < bytes) {
-                    const uint32_t u = V == 4 ? __ldg(reinterpret_cast<const uint32_t*>(row + a))
-                                     : V == 2 ? __ldg(reinterpret_cast<const uint16_t*>(row + a)) : __ldg(reinterpret_cast<const uint8_t*>(row + a));
+                    const uint32_t u = V == 4 ? *reinterpret_cast<const uint32_t*>(row + a)
+                                     : V == 2 ? *reinterpret_cast<const uint16_t*>(row + a) : *reinterpret_cast<const uint8_t*>(row + a);
                     v[i] |= u << (8 * j);
                 }
             }
@@ -65,7 +65,7 @@ __device__ __forceinline__ uint32_t half2_of_e4m3(uint32_t two) {
 
 // A group of `share` warps has `height` rows of w, from n0 on: 4, 8 or kRows.
 template <bool E4M3, int V>
-__global__ void __launch_bounds__(32 * kWarps, 2) linear_few_kernel(const LinearEpilogue e, const char* __restrict__ x, const char* __restrict__ w, int rows, int n_in,
+__global__ void __launch_bounds__(32 * kWarps, 2) linear_few_kernel(const LinearEpilogue e, const char* x, const char* w, int rows, int n_in,
                                                                     int n_out, int share, int height) {
     __shared__ float sums[kWarps][8][kRows];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = warp % share, group = warp / share, groups = kWarps / share;
