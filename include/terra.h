@@ -305,6 +305,7 @@ int terra_rms_norm_workspace_bytes(const terra_norm_desc* desc, size_t* bytes);
 int terra_rms_norm_bwd(const terra_norm_desc* desc, const void* h, const float* weight, const float* rstd, const void* d_y, const void* d_h, void* d_x,
                        float* d_weight, void* workspace, size_t workspace_bytes, void* stream);
 
+/* Of -infinity GELU is 0, its limit; SILU and GELU_TANH are NaN, as the formulas have it.  Slopes at infinities are their limits. */
 #define TERRA_ACT_NONE 0
 #define TERRA_ACT_RELU 1
 #define TERRA_ACT_SILU 2        /* z / (1 + exp(-z)) */

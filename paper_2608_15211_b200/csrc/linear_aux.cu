@@ -99,7 +99,9 @@ __global__ void __launch_bounds__(kBlock) activation_bwd_kernel(const uint16_t* 
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const float2 a = elem2_to_float2(zw[k]), g = elem2_to_float2(gw[k]);
-                out[k] = pack_elem(g.x * act_slope<A>(a.x), g.y * act_slope<A>(a.y));
+                float lo, hi;
+                split_pair(pmul(pair_of(g.x, g.y), act_slope2<A>(pair_of(a.x, a.y))), lo, hi);
+                out[k] = pack_elem(lo, hi);
             }
         });
         *reinterpret_cast<uint4*>(d_z + 8 * i) = make_uint4(out[0], out[1], out[2], out[3]);
