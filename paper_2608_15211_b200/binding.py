@@ -304,9 +304,10 @@ def terra_rms_norm_fwd(x, weight, residual=None, eps=1e-6, h=None, y=None, rstd=
     return (_host or _native()).norm_fwd(x, weight, residual, eps, h, y, rstd)
 
 
-def terra_rms_norm_fwd_e4m3(x, weight, residual=None, eps=1e-6, h=None, y=None, scale=None):
-    """The same with y in 8 bits.  Returns (y float8_e4m3fn like x, scale fp32 [rows], h like x): y stands for y * scale."""
-    return (_host or _native()).norm_fwd_e4m3(x, weight, residual, eps, h, y, scale)
+def terra_rms_norm_fwd_e4m3(x, weight, residual=None, eps=1e-6, h=None, y=None, scale=None, rstd=None):
+    """The same with y in 8 bits.  Returns (y float8_e4m3fn like x, scale fp32 [rows], h like x): y stands for y * scale.  A tensor given as
+    rstd (fp32 [rows]) takes what terra_rms_norm_bwd needs."""
+    return (_host or _native()).norm_fwd_e4m3(x, weight, residual, eps, h, y, scale, rstd)
 
 
 def terra_rms_norm_bwd(h, weight, rstd, d_y, d_h=None, d_x=None, d_weight=None, workspace=None):

@@ -367,18 +367,19 @@ PyObject* norm_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-// x, weight, residual, eps, h, y, scale -> (y, scale, h)
+// x, weight, residual, eps, h, y, scale, rstd (written where it is given) -> (y, scale, h)
 PyObject* norm_fwd_e4m3(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    return guarded(n, 7, [&] {
+    return guarded(n, 8, [&] {
         const at::Tensor &x = tensor(a[0], "x"), &w = tensor(a[1], "weight");
         const terra_norm_desc d = norm_desc(x, w, as_float(a[3]));
         const at::Tensor r = optional(a[2], "residual", x.scalar_type(), x.numel());
-        void *px = ptr(x), *pw = ptr(w), *pr = opt_ptr(r);
+        const at::Tensor rstd = optional(a[7], "rstd", at::kFloat, d.rows);
+        void *px = ptr(x), *pw = ptr(w), *pr = opt_ptr(r), *ps = opt_ptr(rstd);
         at::Tensor h;
         if (r.defined() || a[4] != Py_None) h = result(a[4], "h", x.scalar_type(), x.sizes(), x);
         at::Tensor y = result(a[5], "y", at::kFloat8_e4m3fn, x.sizes(), x);
         at::Tensor scale = result(a[6], "scale", at::kFloat, {d.rows}, x);
-        launch(f_norm_fwd_e4m3, &d, px, pr, (const float*)pw, opt_ptr(h), ptr(y), (float*)ptr(scale), (float*)nullptr, stream());
+        launch(f_norm_fwd_e4m3, &d, px, pr, (const float*)pw, opt_ptr(h), ptr(y), (float*)ptr(scale), (float*)ps, stream());
         return tuple({y, scale, h.defined() ? h : x});
     });
 }
