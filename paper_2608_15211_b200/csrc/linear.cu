@@ -188,11 +188,13 @@ struct Units {
     __device__ __forceinline__ int k1() const { return min(j.k_blocks, (at.split + 1) * j.kb_per_split); }
 };
 
+// The scales one after the other, as for few rows: their product may lie below fp32's normal numbers where the result does not.
+__device__ __forceinline__ Pair scaled2(Pair d, Pair x_scale, Pair w_scale, Pair bias) { return pfma(pmul(d, x_scale), w_scale, bias); }
 // Two neighbouring columns of D to z and y.  `in`: the residual's or the activation input's two elements.
 template <int KIND, int ACT, bool E4M3>
-__device__ __forceinline__ Pair finish2(Pair d, Pair bias, Pair scale, Pair in, Pair& z) {
+__device__ __forceinline__ Pair finish2(Pair d, Pair bias, Pair x_scale, Pair w_scale, Pair in, Pair& z) {
     if (KIND == kLinearInput) return pmul(d, act_slope2<ACT>(in));
-    z = E4M3 ? pfma(d, scale, bias) : padd(d, bias);
+    z = E4M3 ? scaled2(d, x_scale, w_scale, bias) : padd(d, bias);
     return padd(act2<ACT>(z), in);
 }
 __device__ __forceinline__ Pair elems2(uint32_t v) { const float2 t = elem2_to_float2(v); return pair_of(t.x, t.y); }
@@ -306,7 +308,7 @@ __device__ __forceinline__ void finish32(const uint32_t (&acc)[32], const Linear
                     y[i] = pack2(IN ? pmul(d, act_slope2<ACT>(elems2(in[i]))) : d);
                 } else {
                     const Pair bias = pair_of(b[c], b[c + 1]);
-                    const Pair zz = E4M3 ? pfma(d, pmul(both(x_scale), pair_of(w[c], w[c + 1])), bias) : padd(d, bias), a = act2<ACT>(zz);
+                    const Pair zz = E4M3 ? scaled2(d, both(x_scale), pair_of(w[c], w[c + 1]), bias) : padd(d, bias), a = act2<ACT>(zz);
                     y[i] = pack2(IN ? padd(a, elems2(in[i])) : a);
                     if (Z) z[i] = pack2(zz);
                 }
@@ -801,8 +803,8 @@ __device__ __forceinline__ void join4(const LinearEpilogue& e, float (&v)[4], lo
         for (int c = 0; c < 4; c += 2) {
             Pair zz = 0, y;
             const Pair d = pair_of(v[c], v[c + 1]), bb = pair_of(b[c], b[c + 1]), in = pair_of(t[c], t[c + 1]);
-            if (scaled) y = finish2<KIND, decltype(tag)::value, true>(d, bb, pmul(xs, pair_of(w[c], w[c + 1])), in, zz);
-            else y = finish2<KIND, decltype(tag)::value, false>(d, bb, 0, in, zz);
+            if (scaled) y = finish2<KIND, decltype(tag)::value, true>(d, bb, xs, pair_of(w[c], w[c + 1]), in, zz);
+            else y = finish2<KIND, decltype(tag)::value, false>(d, bb, 0, 0, in, zz);
             split_pair(y, v[c], v[c + 1]);
             split_pair(zz, z[c], z[c + 1]);
         }
