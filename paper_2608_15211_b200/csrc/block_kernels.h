@@ -66,7 +66,7 @@ cudaError_t launch_rotary_f16(const RotaryArgs& a, int sm_count, cudaStream_t st
 constexpr int kLinearForward = 0, kLinearInput = 1, kLinearWeights = 2;
 constexpr int kLinearMaxFeatures = 65536;
 constexpr int kLinearChunk = 4;        // weight gradient: stages (of 64 rows) that are summed up in TMEM
-constexpr int kLinearLongChunk = 64;   // the other products: stages (of 64 features, in e4m3 128) that are
+constexpr int kLinearLongChunk = 32;   // the other products: stages (of 64 features, in e4m3 128) that are
 
 // How a product is cut up.  Made for kPlanSms SMs whatever the device has, so that the workspace does not depend on it.
 struct LinearPlan {

@@ -14,8 +14,8 @@
 // The tensor cores' sum over k is cut off, not rounded to nearest, and its error grows with the number of steps, four a stage: 1.9e-8 of the 2-norm a step
 // on N(0, 1), 1.05e-7 where all terms have one sign.  The weight gradient, a sum over all rows that comes out in fp32, therefore leaves TMEM every kLinearChunk
 // stages and is added up in registers (156672 rows of N(0, 1) in fp16: 3.6e-7 off in the 2-norm, with 16 stages 1.2e-6, at the same time).  The other products,
-// whose results are rounded to 16 bits, leave it every kLinearLongChunk stages: terms of one sign are then 2.6e-5 off at most, a nineteenth of fp16's half
-// step.  (65536 features in one go: 4.3e-4.  Every 32 stages 4096 -> 4096 takes 3 % longer for half of the error, every 16 another 1 %, e4m3 with GELU 13 %.)
+// whose results are rounded to 16 bits, leave it every kLinearLongChunk stages: terms of one sign are then 1.3e-5 off at most, a fortieth of fp16's half
+// step.  (4096 features in one go 2.6e-5, 65536 4.3e-4.  156672 x 4096 -> 4096 takes 3399 us instead of 3367 so, with a residual 3538 instead of 3505.)
 //
 // What bounds it: the tensor pipe where the sum is long (156672 x 4096 -> 4096 3.35 ms, 1569 TFLOP/s, the pipe busy in 91 % of the cycles; e4m3 to 16384 with
 // GELU 7.2 ms, 2930 TFLOP/s), over seconds the power cap (4.1 and 9.0 ms); the epilogue where it is short (550800 x 384 -> 1536 with GELU 0.85 ms, two
@@ -286,12 +286,13 @@ __device__ __forceinline__ void copy_tile(uint32_t tile, bool narrow, uint16_t* 
 
 // 32 columns of a thread's row: out of TMEM (`acc`), through the epilogue, into the warp's tile from its 16-byte place `first` on.
 // IN: the places that take y hold the residual or z_in before.  Z: z goes 2 KB behind, or (WIDE) into the next tile.
-template <int KIND, int ACT, bool E4M3, bool IN, bool Z, bool WIDE>
+// READY: scales and bias have been applied.
+template <int KIND, int ACT, bool E4M3, bool IN, bool Z, bool WIDE, bool READY>
 __device__ __forceinline__ void finish32(const uint32_t (&acc)[32], const LinearEpilogue& e, int n, int col, int first, int lane, float x_scale, uint32_t tile) {
 #pragma unroll
     for (int part = 0; part < 2; ++part) {
         float b[16], w[16];
-        if (KIND == kLinearForward) {
+        if (KIND == kLinearForward && !READY) {
             row_values(e.bias ? e.bias : g_no_bias.values, e.bias ? col + 16 * part : 0, e.bias ? n : 64, b);
             if (E4M3) row_values(e.w_scale, col + 16 * part, n, w);
         }
@@ -307,8 +308,8 @@ __device__ __forceinline__ void finish32(const uint32_t (&acc)[32], const Linear
                 if (KIND == kLinearInput) {
                     y[i] = pack2(IN ? pmul(d, act_slope2<ACT>(elems2(in[i]))) : d);
                 } else {
-                    const Pair bias = pair_of(b[c], b[c + 1]);
-                    const Pair zz = E4M3 ? scaled2(d, both(x_scale), pair_of(w[c], w[c + 1]), bias) : padd(d, bias), a = act2<ACT>(zz);
+                    const Pair bias = READY ? 0 : pair_of(b[c], b[c + 1]);
+                    const Pair zz = READY ? d : E4M3 ? scaled2(d, both(x_scale), pair_of(w[c], w[c + 1]), bias) : padd(d, bias), a = act2<ACT>(zz);
                     y[i] = pack2(IN ? padd(a, elems2(in[i])) : a);
                     if (Z) z[i] = pack2(zz);
                 }
@@ -316,6 +317,31 @@ __device__ __forceinline__ void finish32(const uint32_t (&acc)[32], const Linear
             asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(at), "r"(y[0]), "r"(y[1]), "r"(y[2]), "r"(y[3]) : "memory");
             if (KIND == kLinearForward && Z)
                 asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};\n" ::"r"(at + (WIDE ? kTile : kTile / 2)), "r"(z[0]), "r"(z[1]), "r"(z[2]), "r"(z[3]) : "memory");
+        }
+    }
+}
+
+// The same of 64 sums in place, four columns at a time.
+template <bool E4M3>
+__device__ __forceinline__ void scale_and_add(float (&sum)[64], const LinearEpilogue& e, int n, int col, float x_scale) {
+    auto four = [&](const float* p, int at, float (&v)[4]) {
+        if (at + 4 <= n) {
+            const float4 t = *reinterpret_cast<const float4*>(p + at);
+            v[0] = t.x; v[1] = t.y; v[2] = t.z; v[3] = t.w;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = p[min(at + i, n - 1)];
+        }
+    };
+#pragma unroll
+    for (int k = 0; k < 64; k += 4) {
+        float b[4] = {0.f, 0.f, 0.f, 0.f}, w[4];
+        if (e.bias) four(e.bias, col + k, b);
+        if (E4M3) four(e.w_scale, col + k, w);
+#pragma unroll
+        for (int i = 0; i < 4; i += 2) {
+            const Pair d = pair_of(sum[k + i], sum[k + i + 1]), bias = pair_of(b[i], b[i + 1]);
+            split_pair(E4M3 ? scaled2(d, both(x_scale), pair_of(w[i], w[i + 1]), bias) : padd(d, bias), sum[k + i], sum[k + i + 1]);
         }
     }
 }
@@ -351,7 +377,8 @@ __device__ __forceinline__ void write_sums(uint32_t tile, float* out, long long 
 // MAP: the rows of the outputs (and of the residual or z_in) are multiples of 16 bytes and the copy engine moves them; else the warps do.  (One kernel with
 // both spilled registers around the warps' copies: 2203200 x 256 -> 384 558 -> 1032 us.)
 // LONG: the sum leaves TMEM every kLinearLongChunk stages, for sums that have more.  (An instantiation of its own: the 64 sums that a thread holds spill
-// registers around the epilogue.)
+// registers around the epilogue, and what is spilled takes the way to memory that the products' operands take.  Scales and bias go to the sums in place, four
+// columns at a time: with 16 of them in registers, as elsewhere, 4096 -> 4096 took 4 % longer, 8448 -> 4096 in e4m3 8 %.)
 template <bool PAIR, int KIND, bool E4M3, bool MAP, int TILES, bool LONG>
 __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Job job) {
     static_assert(!LONG || TILES == 1, "two tiles a warp are for short sums");
@@ -676,8 +703,14 @@ __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_consta
                     const int col0 = 64 * chunk, col = n0 + col0, cols = min(64, job.bn - col0), own = min(cols, job.N - col);
                     float x_scale = 1.f;
                     if (E4M3 && lane < rows) x_scale = job.e.x_scale[row0 + lane];
+                    if constexpr (LONG && KIND == kLinearForward) scale_and_add<E4M3>(sum, job.e, job.N, col, x_scale);
+                    auto shift = [&] {                 // the sums of the next 32 columns take the place of those that are done
+                        if constexpr (LONG)
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) sum[i] = sum[i + 32];
+                    };
 #pragma unroll 1
-                    for (int p0 = 0; p0 < cols; p0 += 32) {
+                    for (int p0 = 0; p0 < cols; p0 += 32, shift()) {
                         if (p0 == 0 || width == 32) {          // a new tile
                             if (lane == 0 && p0 > 0) prepare(row0, col + p0, t);
                             __syncwarp();
@@ -709,10 +742,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_consta
                         uint32_t cur[32];
                         if constexpr (LONG) {
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) {
-                                cur[i] = __float_as_uint(sum[i]);
-                                sum[i] = sum[i + 32];  // the next 32 columns
-                            }
+                            for (int i = 0; i < 32; ++i) cur[i] = __float_as_uint(sum[i]);
                         } else {
                             tmem_ld32(acc + col0 + p0, cur);
                             tmem_ld_wait();
@@ -724,10 +754,10 @@ __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_consta
                         with_act(job.e.activation, [&](auto tag) {
                             constexpr int ACT = decltype(tag)::value;
                             constexpr bool W = TILES == 2;
-                            if (TILES == 1 && has_z && has_in) finish32<KIND, ACT, E4M3, true, true, W>(cur, job.e, job.N, col + p0, 0, lane, x_scale, to);
-                            else if (has_z) finish32<KIND, ACT, E4M3, false, true, W>(cur, job.e, job.N, col + p0, W ? p0 >> 3 : 0, lane, x_scale, to);
-                            else if (has_in) finish32<KIND, ACT, E4M3, true, false, W>(cur, job.e, job.N, col + p0, p0 >> 3, lane, x_scale, to);
-                            else finish32<KIND, ACT, E4M3, false, false, W>(cur, job.e, job.N, col + p0, p0 >> 3, lane, x_scale, to);
+                            if (TILES == 1 && has_z && has_in) finish32<KIND, ACT, E4M3, true, true, W, LONG>(cur, job.e, job.N, col + p0, 0, lane, x_scale, to);
+                            else if (has_z) finish32<KIND, ACT, E4M3, false, true, W, LONG>(cur, job.e, job.N, col + p0, W ? p0 >> 3 : 0, lane, x_scale, to);
+                            else if (has_in) finish32<KIND, ACT, E4M3, true, false, W, LONG>(cur, job.e, job.N, col + p0, p0 >> 3, lane, x_scale, to);
+                            else finish32<KIND, ACT, E4M3, false, false, W, LONG>(cur, job.e, job.N, col + p0, p0 >> 3, lane, x_scale, to);
                         });
                         if (width == 64 && p0 + 32 < cols) continue;
                         const int at0 = width == 32 ? p0 : 0;  // the tile's first column
