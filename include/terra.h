@@ -41,7 +41,7 @@ typedef enum {
     TERRA_ERR_INVALID_ARG = 1,   /* null pointer, non-positive size, element count out of range   */
     TERRA_ERR_UNSUPPORTED = 2,   /* head_dim not in {32, 64, 128}, window, channels or features too large, not an sm_100 GPU */
     TERRA_ERR_ALIGNMENT = 3,     /* a pointer is not 16-byte aligned                              */
-    TERRA_ERR_WORKSPACE = 4,     /* workspace NULL or smaller than terra_swin_workspace_bytes     */
+    TERRA_ERR_WORKSPACE = 4,     /* workspace NULL or smaller than the call's terra_*_workspace_bytes */
     TERRA_ERR_CUDA = 5,          /* a CUDA call failed; text via terra_last_cuda_error            */
     TERRA_ERR_DEVICE_TIMEOUT = 6,/* a bounded wait inside a kernel expired (see terra_swin_check) */
     TERRA_ERR_NOALLOC_LIMIT = 7  /* terra_swin_attn_fwd_noalloc: more heads than its fixed scratch holds */

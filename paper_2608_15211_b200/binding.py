@@ -1,6 +1,6 @@
 """Thin Python binding of the C ABI declared in include/terra.h.
 
-Argument marshalling only (the attention calls' in native code, csrc/host_module.cpp): tensors must already live on the GPU; every step of the path
+Argument marshalling only (the attention calls' and those around them in native code, csrc/host_module.cpp): tensors must already live on the GPU; every step of the path
 (route, gather, attention, scatter) runs in the library's kernels.  There is no CPU
 fallback: if the shared library is missing or no CUDA device is present, calls raise.
 PyTorch is used for device memory and streams.
@@ -117,7 +117,7 @@ _host = None
 
 
 def _bind_host(lib) -> None:
-    """The native module that checks and marshals the attention calls' arguments gets the library's entry points."""
+    """The native module that checks and marshals the calls' arguments gets the library's entry points."""
     global _host
     if not os.path.exists(HOST_PATH):
         raise FileNotFoundError(f"{HOST_PATH} not found: build it with `python -m paper_2608_15211_b200.build`")

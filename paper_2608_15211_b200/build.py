@@ -46,7 +46,7 @@ def _host_stale() -> bool:
 
 
 def build_host(force: bool = False) -> str:
-    """Compile csrc/host_module.cpp, the attention calls' argument handling, against the installed Python and torch."""
+    """Compile csrc/host_module.cpp, the calls' argument handling, against the installed Python and torch."""
     if not force and not _host_stale():
         return HOST_PATH
     import torch

@@ -410,7 +410,7 @@ const char* terra_strerror(int status) {
         case TERRA_ERR_INVALID_ARG: return "invalid argument (null pointer, non-positive size, or size out of range)";
         case TERRA_ERR_UNSUPPORTED: return "unsupported configuration (head_dim must be 32, 64 or 128, window <= 128, norm channels <= 16384, product features <= 65536, GPU must be sm_100)";
         case TERRA_ERR_ALIGNMENT: return "pointer is not 16-byte aligned";
-        case TERRA_ERR_WORKSPACE: return "workspace missing or too small (see terra_swin_workspace_bytes)";
+        case TERRA_ERR_WORKSPACE: return "workspace missing or too small (see terra_swin_workspace_bytes, terra_rms_norm_workspace_bytes, terra_linear_workspace_bytes)";
         case TERRA_ERR_CUDA: return "CUDA error (see terra_last_cuda_error)";
         case TERRA_ERR_DEVICE_TIMEOUT: return "a bounded wait inside a kernel expired; results of that call are invalid";
         case TERRA_ERR_NOALLOC_LIMIT: return "terra_swin_attn_fwd_noalloc: heads exceeds TERRA_NOALLOC_MAX_HEADS, the size of its fixed scratch";

@@ -200,7 +200,8 @@ rms_norm_fwd_kernel(const NormArgs a, int lanes, int lanes_log2) {
 
 // n = h rstd, g = d_y weight: dx = rstd (g - n mean(g n)) + d_h, dweight = sum over the rows of d_y n.  A block adds up its rows'
 // dweight in registers and writes one row of `partial`; sum_partials_kernel adds those in a fixed order.
-// What bounds it: HBM (156672 x 4096 807 us, 131072 x 768 135 us, 6.0 to 6.4 TB/s).
+// What bounds it: HBM (156672 x 4096 806 us, 131072 x 768 134 us, 6.0 to 6.4 TB/s); where the registers of a row's four vectors, or of its single elements and
+// pairs, spill and leave none for the next row, what is spilled and the wait for a row's reads (40000 x 16384 1549 us, 3.4 TB/s; 300000 x 1001 968 us, 2.5 TB/s).
 template <int E, int V>
 __global__ void __launch_bounds__(kMaxLanes)
 rms_norm_bwd_kernel(const NormArgs a, int lanes, int lanes_log2) {

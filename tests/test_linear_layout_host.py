@@ -4,7 +4,8 @@ import re
 
 import pytest
 
-from paper_2608_15211_b200.build import CSRC
+from paper_2608_15211_b200 import binding
+from paper_2608_15211_b200.build import CSRC, build
 from tests._host_program import run_host_program
 
 
@@ -28,3 +29,10 @@ def test_dependent_launches_read_by_plain_loads(name):
     assert kernels
     for kernel, arguments in kernels:
         assert "__restrict__" not in arguments, kernel
+
+
+def test_a_missing_workspace_names_every_call_that_asks_for_one():
+    build()
+    lib = binding.load_library()
+    text = lib.terra_strerror(4).decode()
+    assert all(n in text for n in binding.EXPORTS if n.endswith("_workspace_bytes"))
