@@ -17,8 +17,8 @@
 // whose results are rounded to 16 bits, leave it every kLinearLongChunk stages: terms of one sign are then 1.3e-5 off at most, a fortieth of fp16's half
 // step.  (4096 features in one go 2.6e-5, 65536 4.3e-4.  156672 x 4096 -> 4096 takes 3399 us instead of 3367 so, with a residual 3538 instead of 3505.)
 //
-// What bounds it: the tensor pipe where the sum is long (156672 x 4096 -> 4096 3.35 ms, 1569 TFLOP/s, the pipe busy in 91 % of the cycles; e4m3 to 16384 with
-// GELU 7.2 ms, 2930 TFLOP/s), over seconds the power cap (4.1 and 9.0 ms); the epilogue where it is short (550800 x 384 -> 1536 with GELU 0.85 ms, two
+// What bounds it: the tensor pipe where the sum is long (156672 x 4096 -> 4096 3.40 ms, 1546 TFLOP/s, the pipe busy in 89 % of the cycles; e4m3 to 16384 with
+// GELU 7.2 ms, 2920 TFLOP/s), over seconds the power cap (4.1 and 9.0 ms); the epilogue where it is short (550800 x 384 -> 1536 with GELU 0.85 ms, two
 // reciprocals or exponentials an output in a unit that takes 16 a clock and SM, busy in half the cycles), with z besides the writes: 3.4 GB, of which HBM
 // takes 3.9 GB a ms (0.98 ms).  Rows that are no multiples of 16 bytes: the warps' copies (2203200 x 256 -> 372 0.64 ms, -> 384 0.56).
 //
