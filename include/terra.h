@@ -300,7 +300,8 @@ int terra_rms_norm_fwd_e4m3(const terra_norm_desc* desc, const void* x, const vo
 int terra_rms_norm_fwd_i8(const terra_norm_desc* desc, const void* x, const void* residual, const float* weight, void* h, void* y8, float* scale,
                           float* rstd, void* stream);
 /*
- * The same of x itself, without a norm: rows of tokens, or the rows of a weight matrix (one scale for each output).  1 <= channels <= 65536.
+ * The same of x itself, without a norm: rows of tokens, or the rows of a weight matrix (one scale for each output): x8 = 127 x / max over the row of |x|
+ * rounded to the nearest whole number, ties to the even one (no error of the quotient or the scale moves one).  1 <= channels <= 65536.
  *   x       elem [rows, channels], `dtype` TERRA_DTYPE_*
  *   x8      int8 [rows, channels]
  *   scale   fp32 [rows]

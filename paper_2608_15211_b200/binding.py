@@ -336,7 +336,7 @@ def terra_rms_norm_fwd_i8(x, weight, residual=None, eps=1e-6, h=None, y=None, sc
 
 
 def terra_quantize_i8(x, x8=None, scale=None):
-    """Rows of x (bf16 or fp16 [..., channels], tokens or the outputs of a weight matrix) in 8-bit integers with a scale each, max / 127.
+    """Rows of x (bf16 or fp16 [..., channels], tokens or the outputs of a weight matrix) in 8-bit integers with a scale each, max / 127; ties go to even.
     Returns (x8 int8 like x, scale fp32 [rows])."""
     return (_host or _native()).quantize_i8(x, x8, scale)
 

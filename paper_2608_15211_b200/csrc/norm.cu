@@ -51,6 +51,23 @@ __device__ __forceinline__ float far_out(float y, float scale) {
     return OUT == kOpsI8 && fabsf(q) > kI8Max ? copysignf(kI8Max, q) : q;
 }
 
+// Rows of the activations' type in whole numbers: 127 x / max to the nearest one, ties to the even one.  Of numbers of 11 bits at most, a quotient that is no
+// tie is 2^-19 of itself away from one (254 X and an odd multiple of M differ by 1 at least, and 254 X is below 2^19), and ties are numbers that fp32 holds: the quotient to half a step of fp32
+// decides both.  That takes the reciprocal to twice fp32's digits, hi + lo; with hi alone x = max / 2, 63.5, went to 63 or 64 as the row's reciprocal was rounded.
+// Far out the row is scaled by a power of two first, so that lo stays among the normal numbers.  A row that is not finite gives zeros.
+struct Whole {
+    float pre, hi, lo;
+    __device__ __forceinline__ explicit Whole(float top) {
+        pre = top < 0x1p-60f ? 0x1p100f : top > 0x1p60f ? 0x1p-64f : 1.f;
+        const float m = top * pre;
+        hi = kI8Max * fast_rcp(m);
+        lo = fmaf(-hi, m, kI8Max) * (hi * (1.f / kI8Max));
+        if (!(m > 0.f && m < INFINITY)) hi = lo = 0.f;
+    }
+    __device__ __forceinline__ bool near() const { return pre == 1.f && hi > 0.f; }
+    __device__ __forceinline__ float operator()(float x) const { return fmaf(x * pre, hi, x * pre * lo); }       // (not finite: 0 or NaN, of which the whole number is 0)
+};
+
 // Sum (or maximum) over the threads of a row, to all of them.  `turn` alternates the two halves of `buf` (32 floats each): one
 // barrier a reduction is enough, since a half is written again only after the next reduction's barrier.
 template <bool MAX>
@@ -143,7 +160,16 @@ rms_norm_fwd_kernel(const NormArgs a, int lanes, int lanes_log2) {
             const float scale = top / (OUT == kOpsI8 ? kI8Max : kE4m3Max);
             if (live && lane == 0) a.scale[row] = scale;
             const float by = rstd / scale;             // y / scale = f weight by
-            if (scale >= 0x1p-100f && by < 0x1p100f) {
+            if (!NORM) {
+                const Whole whole(top);
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const int c = lane + v * lanes;
+#pragma unroll
+                    for (int e = 0; e < E; ++e) f[v][e] = whole(f[v][e]);
+                    if (live && c < chunks) store_8<OUT>((uint8_t*)a.y + at + c * E, f[v]);
+                }
+            } else if (scale >= 0x1p-100f && by < 0x1p100f) {
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
                     const int c = lane + v * lanes;
@@ -189,7 +215,7 @@ __device__ __forceinline__ uint32_t max_elem2(uint32_t a, uint32_t b) {
 
 // Rows quantised, up to V vectors of 8 to a thread.  A thread has all of its reads under way at once and keeps them as they are, so that many fit: what
 // bounds it is HBM behind that.  (156672 x 4096, the norm's kernel without the norm, two vectors a thread and the next row's two ahead: 515 us.)
-// Where x by is a number that fp32 holds with its whole part, x by + 1.5 2^23 has the nearest whole number in its last byte.
+// A quotient + 1.5 2^23 has the nearest whole number in its last byte.
 template <int V>
 __global__ void __launch_bounds__(kBlock, V == 8 ? 4 : V == 4 ? 5 : 6) quantize_kernel(const NormArgs a, int lanes, int lanes_log2) {
     __shared__ float buf[64];
@@ -215,24 +241,32 @@ __global__ void __launch_bounds__(kBlock, V == 8 ? 4 : V == 4 ? 5 : 6) quantize_
             most = max_elem2(max_elem2(max_elem2(r[v].v.x & m, r[v].v.y & m), max_elem2(r[v].v.z & m, r[v].v.w & m)), most);
         }
         const float2 two = elem2_to_float2(most);
-        const float scale = over_row<true>(max_nan(two.x, two.y), lanes, buf, turn) / kI8Max, by = 1.f / scale;
-        if (live && lane == 0) a.scale[row] = scale;
-        const bool plain = scale >= 0x1p-100f && scale < INFINITY;
+        const float top = over_row<true>(max_nan(two.x, two.y), lanes, buf, turn);
+        if (live && lane == 0) a.scale[row] = top / kI8Max;
+        const Whole whole(top);
+        const Pair hi = both(whole.hi), lo = both(whole.lo);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int c = lane + v * lanes;
             if (!live || c >= chunks) continue;
-            float f[8];
-            r[v].floats(f);
-            if (plain) {
+            if (whole.near()) {
+                Pair p[4];
+                r[v].pairs(p);
                 uint32_t q[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) q[e] = __float_as_uint(fmaf(f[e], by, 12582912.f));
+                for (int i = 0; i < 4; ++i) {
+                    float a0, a1;
+                    split_pair(padd(pfma(p[i], hi, pmul(p[i], lo)), both(12582912.f)), a0, a1);
+                    q[2 * i] = __float_as_uint(a0);
+                    q[2 * i + 1] = __float_as_uint(a1);
+                }
                 *reinterpret_cast<uint2*>(y + c * 8) = make_uint2(__byte_perm(__byte_perm(q[0], q[1], 0x40), __byte_perm(q[2], q[3], 0x40), 0x5410),
                                                                   __byte_perm(__byte_perm(q[4], q[5], 0x40), __byte_perm(q[6], q[7], 0x40), 0x5410));
             } else {
+                float f[8];
+                r[v].floats(f);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) f[e] = far_out<kOpsI8>(f[e], scale);
+                for (int e = 0; e < 8; ++e) f[e] = whole(f[e]);
                 store_8<kOpsI8>(y + c * 8, f);
             }
         }
@@ -258,17 +292,15 @@ __global__ void __launch_bounds__(kMaxLanes) quantize_wide_kernel(const NormArgs
             for (int e = 0; e < E; ++e) top = max_nan(top, fabsf(f[e]));
         }
         top = over_row<true>(top, kMaxLanes, buf, turn);
-        const float scale = top / kI8Max;
-        if (threadIdx.x == 0) a.scale[row] = scale;
-        const float by = 1.f / scale;
-        const bool far = !(scale >= 0x1p-100f);
+        if (threadIdx.x == 0) a.scale[row] = top / kI8Max;
+        const Whole whole(top);
         for (int c = threadIdx.x; c < chunks; c += kMaxLanes) {
             Raw<E> r;
             r.load(x + c * E);
             float f[E];
             r.floats(f);
 #pragma unroll
-            for (int e = 0; e < E; ++e) f[e] = far ? far_out<kOpsI8>(f[e], scale) : f[e] * by;
+            for (int e = 0; e < E; ++e) f[e] = whole(f[e]);
             store_8<kOpsI8>(y + c * E, f);
         }
     }
