@@ -467,7 +467,8 @@ __global__ void __launch_bounds__(1024) group_bwd_join_kernel(const __grid_const
     if (cx == 0 && w < n) p.sums[(long long)(p.first + blockIdx.y) * n + w] = s;
 }
 
-// The terms of group g's d_x, -rstd mean(g weight) and -rstd^3 mean(g weight (x - mean)), of its channels' sums (two of each); by a warp.
+// The terms of group g's d_x, -rstd mean(g weight) and -rstd mean(g weight n), of its channels' sums (two of each); by a warp.  (The sum goes through
+// g weight (x - mean): rstd comes to it factor by factor, so that nothing leaves fp32's range that is not there in d_x.)
 __device__ __forceinline__ void group_means(const Pass& p, const Place& a, int g, const float* sums, float* out, int lane) {
     float l = 0.f, m = 0.f;
     for (int c = g * p.per_group + lane; c < (g + 1) * p.per_group; c += 32) {
@@ -483,20 +484,23 @@ __device__ __forceinline__ void group_means(const Pass& p, const Place& a, int g
     if (lane) return;
     const float rstd = p.stats[2 * ((long long)a.sample * p.groups + g) + 1], by = (float)p.per_value;
     out[0] = -rstd * (l * by);
-    out[1] = -rstd * rstd * rstd * (m * by);
+    out[1] = -(rstd * (rstd * (m * by)));
 }
 template <int E>
-__device__ __forceinline__ void group_terms(const Pass& p, const Place& a, const float* group_sums, Pair (&c0)[Channels<E>::kPairs], Pair (&c1)[Channels<E>::kPairs]) {
+__device__ __forceinline__ void group_terms(const Pass& p, const Place& a, const float* group_sums, Pair (&c0)[Channels<E>::kPairs], Pair (&c1)[Channels<E>::kPairs],
+                                            Pair (&rstd)[Channels<E>::kPairs]) {
     const int g0 = a.s0 / p.per_group;
+    const float* stats = p.stats + 2 * ((long long)a.sample * p.groups + g0) + 1;
 #pragma unroll
     for (int i = 0; i < Channels<E>::kPairs; ++i) {
         const int lo = 2 * ((a.c0 + 2 * i) / p.per_group - g0), hi = E > 1 ? 2 * ((a.c0 + 2 * i + 1) / p.per_group - g0) : lo;
         c0[i] = pair_of(group_sums[lo], group_sums[hi]);
         c1[i] = pair_of(group_sums[lo + 1], group_sums[hi + 1]);
+        rstd[i] = pair_of(stats[lo], stats[hi]);
     }
 }
 
-// Second pass: d_x = a g + c0 + (x - mean) c1 with c0 = - rstd mean(g weight), c1 = - rstd^2 mean(g weight n) of the group (rstd of its own in n).
+// Second pass: d_x = a g + c0 + (x - mean) rstd c1 with c0 = - rstd mean(g weight), c1 = - rstd mean(g weight n) of the group.
 // The last launch's blocks also add up the sums of a few samples: d_weight and d_bias.
 template <int E>
 __global__ void __launch_bounds__(kBlock, blocks(E, 2)) group_bwd_apply_kernel(const __grid_constant__ Pass p) {
@@ -523,10 +527,10 @@ __global__ void __launch_bounds__(kBlock, blocks(E, 2)) group_bwd_apply_kernel(c
             p.d_bias[c] = b;
         }
     }
-    Pair c0[kPairs], c1[kPairs];
+    Pair c0[kPairs], c1[kPairs], rstd[kPairs];
 #pragma unroll
-    for (int i = 0; i < kPairs; ++i) c0[i] = c1[i] = both(0.f);
-    if (a.there) group_terms<E>(p, a, group_sums, c0, c1);
+    for (int i = 0; i < kPairs; ++i) c0[i] = c1[i] = rstd[i] = both(0.f);
+    if (a.there) group_terms<E>(p, a, group_sums, c0, c1, rstd);
     with_act(p.activation, [&](auto tag) {
         walk<E, 2, kStagesBwd, true>(p, a, shared, [&](const Raw<E> (&x)[deep(E, 2)], const Raw<E> (&d_y)[deep(E, 2)], int n, long long at, int step) {
             each_token<deep(E, 2)>(n, [&](int k) {
@@ -537,7 +541,7 @@ __global__ void __launch_bounds__(kBlock, blocks(E, 2)) group_bwd_apply_kernel(c
                 for (int i = 0; i < kPairs; ++i) {
                     const Pair d = padd(v[i], ch.minus_mean[i]);
                     const Pair gg = pmul(g[i], finite_slope2<decltype(tag)::value>(pfma(d, ch.a[i], ch.b[i])));
-                    v[i] = pfma(gg, ch.a[i], pfma(d, c1[i], c0[i]));
+                    v[i] = pfma(gg, ch.a[i], pfma(pmul(d, rstd[i]), c1[i], c0[i]));
                 }
                 store_pairs<E>(p.out + at + (long long)k * step, v);
             });
@@ -779,12 +783,12 @@ __global__ void __launch_bounds__(kBlock, 2) group_small_bwd_kernel(const __grid
     for (int g = warp; g < groups; g += kBlock / 32) group_means(p, a, g + a.s0 / p.per_group, total - 2 * a.s0, group_sums + 2 * g, lane);
     __syncthreads();
     if (n) {
-        Pair c0[kPairs], c1[kPairs];
-        group_terms<E>(p, a, group_sums, c0, c1);
+        Pair c0[kPairs], c1[kPairs], rstd[kPairs];
+        group_terms<E>(p, a, group_sums, c0, c1, rstd);
         with_act(p.activation, [&](auto tag) {
             each_held<KEEP>(n, [&](int k) {
                 Pair v[kPairs];
-                slope(tag, k, [&](int i, Pair d, Pair g) { v[i] = pfma(g, ch.a[i], pfma(d, c1[i], c0[i])); });
+                slope(tag, k, [&](int i, Pair d, Pair g) { v[i] = pfma(g, ch.a[i], pfma(pmul(d, rstd[i]), c1[i], c0[i])); });
                 store_pairs<E>(p.out + from + k * step, v);
             });
         });
