@@ -55,19 +55,8 @@ __device__ __forceinline__ void join4(const LinearEpilogue& e, float (&v)[4], lo
             }
     }
 }
-__device__ __forceinline__ void part4(const float* p, int col, int N, float (&v)[4]) {       // adds four columns of a part
-    if ((N & 3) == 0) {
-        const float4 t = *reinterpret_cast<const float4*>(p);
-        v[0] += t.x; v[1] += t.y; v[2] += t.z; v[3] += t.w;
-    } else {
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-            if (col + c < N) v[c] += p[c];
-    }
-}
-
-// Joins the parts of a split product: the sum over the splits, in a fixed order, then the epilogue.
-template <int KIND>
+// Joins the parts of a split product: the sum over the splits, in a fixed order, then the epilogue.  WHOLE: parts in 32-bit integers.
+template <int KIND, bool WHOLE>
 __global__ void __launch_bounds__(256) linear_join_kernel(const LinearEpilogue e, const float* parts, int splits, long long M, int N, float* out,
                                                           const float* a_parts, int a_splits) {
     let_dependents_start();
@@ -86,22 +75,24 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const LinearEpilogue e
         long long row;
         int c4;
         split_item(i, per_row, row, c4);
-        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        typename SumOf<WHOLE>::Type v[4] = {0, 0, 0, 0};
 #pragma unroll 8
-        for (int s = 0; s < splits; ++s) part4(parts + s * part + (size_t)row * N + 4 * c4, 4 * c4, N, v);
-        join4<KIND>(e, v, row, 4 * c4, N, out);
+        for (int s = 0; s < splits; ++s) part4<WHOLE>(parts + s * part + (size_t)row * N + 4 * c4, 4 * c4, N, v);
+        float f[4] = {(float)v[0], (float)v[1], (float)v[2], (float)v[3]};
+        join4<KIND>(e, f, row, 4 * c4, N, out);
     }
 }
 // The same for outputs too small to fill the device so: 8 threads share the parts of four columns.  (A thread that adds 64 parts up alone waits for
 // memory eight times.)  Blocks from `quads` on add up a_parts.
-template <int KIND>
+template <int KIND, bool WHOLE>
 __global__ void __launch_bounds__(256) linear_join_small_kernel(const LinearEpilogue e, const float* parts, int splits, long long M, int N, float* out,
                                                                 const float* a_parts, int a_splits, int quads) {
-    __shared__ float sums[8][32][4];
+    typedef typename SumOf<WHOLE>::Type Sum;
+    __shared__ Sum sums[8][32][4];
     let_dependents_start();
     wait_for_prerequisites();
     const int sub = threadIdx.x >> 5, lane = threadIdx.x & 31, per_row = (N + 3) / 4;
-    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    Sum v[4] = {0, 0, 0, 0};
     const bool is_a = KIND == kLinearWeights && (int)blockIdx.x >= quads;
     const long long i = (is_a ? blockIdx.x - quads : blockIdx.x) * 32ll + lane;
     long long row = 0;
@@ -113,7 +104,7 @@ __global__ void __launch_bounds__(256) linear_join_small_kernel(const LinearEpil
     } else if (i < M * per_row) {
         split_item(i, per_row, row, c4);
 #pragma unroll 4
-        for (int s = sub; s < splits; s += 8) part4(parts + s * (size_t)M * N + (size_t)row * N + 4 * c4, 4 * c4, N, v);
+        for (int s = sub; s < splits; s += 8) part4<WHOLE>(parts + s * (size_t)M * N + (size_t)row * N + 4 * c4, 4 * c4, N, v);
     }
 #pragma unroll
     for (int c = 0; c < 4; ++c) sums[sub][lane][c] = v[c];
@@ -126,7 +117,8 @@ __global__ void __launch_bounds__(256) linear_join_small_kernel(const LinearEpil
     if (is_a) {
         if (i < M) e.a_sums[i] = v[0];
     } else if (i < M * per_row) {
-        join4<KIND>(e, v, row, 4 * c4, N, out);
+        float f[4] = {(float)v[0], (float)v[1], (float)v[2], (float)v[3]};
+        join4<KIND>(e, f, row, 4 * c4, N, out);
     }
 }
 
@@ -220,11 +212,13 @@ cudaError_t launch_linear(int kind, int ops, const LinearPlan& p, long long M, i
     const float* ap = a_splits ? (const float*)a_parts : nullptr;
     prof_begin("linear_join_kernel", stream);
     if (splits_are_many(p.splits, quads)) {
-        auto join = kind == kLinearForward ? linear_join_small_kernel<kLinearForward> : kind == kLinearInput ? linear_join_small_kernel<kLinearInput> : linear_join_small_kernel<kLinearWeights>;
+        auto join = kind == kLinearWeights ? linear_join_small_kernel<kLinearWeights, false> : kind == kLinearInput ? linear_join_small_kernel<kLinearInput, false>
+                  : ops == kOpsI8          ? linear_join_small_kernel<kLinearForward, true>  : linear_join_small_kernel<kLinearForward, false>;
         const unsigned blocks = (unsigned)((quads + 31) / 32);
         e = launch_dependent(join, blocks + (ap ? (unsigned)((M + 31) / 32) : 0u), 256u, 0, stream, epi, (const float*)parts, p.splits, M, N, out, ap, a_splits, (int)blocks);
     } else {
-        auto join = kind == kLinearForward ? linear_join_kernel<kLinearForward> : kind == kLinearInput ? linear_join_kernel<kLinearInput> : linear_join_kernel<kLinearWeights>;
+        auto join = kind == kLinearWeights ? linear_join_kernel<kLinearWeights, false> : kind == kLinearInput ? linear_join_kernel<kLinearInput, false>
+                  : ops == kOpsI8          ? linear_join_kernel<kLinearForward, true>  : linear_join_kernel<kLinearForward, false>;
         const long long need = (quads + 255) / 256, fit = 8ll * sm_count;
         e = launch_dependent(join, (unsigned)(need < fit ? need : fit), 256u, 0, stream, epi, (const float*)parts, p.splits, M, N, out, ap, a_splits);
     }

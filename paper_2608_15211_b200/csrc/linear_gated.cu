@@ -20,12 +20,13 @@ namespace terra {
 namespace {
 
 // Joins the parts of a split product, in a fixed order: four neighbouring columns to 8 threads, which share the parts.  BWD: `parts` [splits][M][N] of d;
-// forward [splits][2][M][N], gate and up.
+// forward [splits][2][M][N], gate and up.  WHOLE: parts in 32-bit integers.
 constexpr int kJoinShare = 8, kJoinQuads = 32;
-template <bool BWD>
+template <bool BWD, bool WHOLE>
 __global__ void __launch_bounds__(kJoinShare * kJoinQuads) gated_join_kernel(const LinearEpilogue e, const float* parts, int splits, long long M, int N) {
     constexpr int H = BWD ? 1 : 2;
-    __shared__ float sums[kJoinShare][H][kJoinQuads][4];
+    typedef typename SumOf<WHOLE>::Type Sum;
+    __shared__ Sum sums[kJoinShare][H][kJoinQuads][4];
     let_dependents_start();
     wait_for_prerequisites();
     const int sub = threadIdx.x / kJoinQuads, lane = threadIdx.x % kJoinQuads, per_row = (N + 3) / 4;
@@ -35,23 +36,12 @@ __global__ void __launch_bounds__(kJoinShare * kJoinQuads) gated_join_kernel(con
     int c4 = 0;
     if (there) split_item(i, per_row, row, c4);
     const int col = 4 * c4;
-    const bool wide = (N & 3) == 0;
 #pragma unroll
     for (int h = 0; h < H; ++h) {
-        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        Sum v[4] = {0, 0, 0, 0};
         if (there)
 #pragma unroll 4
-            for (int s = sub; s < splits; s += kJoinShare) {
-                const float* p = parts + ((long long)s * H + h) * part + row * N + col;
-                if (wide) {
-                    const float4 t = *reinterpret_cast<const float4*>(p);
-                    v[0] += t.x; v[1] += t.y; v[2] += t.z; v[3] += t.w;
-                } else {
-#pragma unroll
-                    for (int c = 0; c < 4; ++c)
-                        if (col + c < N) v[c] += p[c];
-                }
-            }
+            for (int s = sub; s < splits; s += kJoinShare) part4<WHOLE>(parts + ((long long)s * H + h) * part + row * N + col, col, N, v);
 #pragma unroll
         for (int c = 0; c < 4; ++c) sums[sub][h][lane][c] = v[c];
     }
@@ -61,9 +51,10 @@ __global__ void __launch_bounds__(kJoinShare * kJoinQuads) gated_join_kernel(con
     float v[H];
 #pragma unroll
     for (int h = 0; h < H; ++h) {
-        v[h] = 0.f;
+        Sum sum = 0;
 #pragma unroll
-        for (int s = 0; s < kJoinShare; ++s) v[h] += sums[s][h][lane][sub];
+        for (int s = 0; s < kJoinShare; ++s) sum += sums[s][h][lane][sub];
+        v[h] = (float)sum;
     }
     const int n = col + sub;
     const long long g_at = row * 2 * N + n, u_at = g_at + N;
@@ -127,10 +118,10 @@ cudaError_t launch_tiles(bool pair, const Maps& maps, Job& job, int sm_count, cu
 }
 
 template <bool BWD>
-cudaError_t join(cudaError_t e, const LinearPlan& p, const LinearEpilogue& epi, const float* parts, long long M, int N, cudaStream_t stream) {
+cudaError_t join(cudaError_t e, int ops, const LinearPlan& p, const LinearEpilogue& epi, const float* parts, long long M, int N, cudaStream_t stream) {
     if (e != cudaSuccess || p.splits == 1) return e;
     prof_begin("gated_join_kernel", stream);
-    e = launch_dependent(gated_join_kernel<BWD>, (unsigned)((M * ((N + 3) / 4) + kJoinQuads - 1) / kJoinQuads), (unsigned)(kJoinShare * kJoinQuads), 0, stream, epi, parts, p.splits,
+    e = launch_dependent(!BWD && ops == kOpsI8 ? gated_join_kernel<BWD, !BWD> : gated_join_kernel<BWD, false>, (unsigned)((M * ((N + 3) / 4) + kJoinQuads - 1) / kJoinQuads), (unsigned)(kJoinShare * kJoinQuads), 0, stream, epi, parts, p.splits,
                          M, N);
     count_launch(stream);
     return e;
@@ -173,7 +164,7 @@ cudaError_t launch_gated(int ops, const LinearPlan& p, long long M, int N, long 
     else if (!map) e = launch_tiles<kLinearGated, kOps16, false, 3>(p.pair, maps, job, sm_count, stream);
     else if (epi.z && p.splits == 1) e = launch_tiles<kLinearGated, kOps16, true, 3>(p.pair, maps, job, sm_count, stream);
     else e = launch_tiles<kLinearGated, kOps16, true, 1>(p.pair, maps, job, sm_count, stream);
-    return join<false>(e, p, epi, parts, M, N, stream);
+    return join<false>(e, ops, p, epi, parts, M, N, stream);
 }
 
 // [d u act'(g), d act(g)] with d = d_z w, of z_in = [g, u]; d_z [M][K], w [K][N], z_in and the result [M][2 N]
@@ -194,7 +185,7 @@ cudaError_t launch_gated_input(const LinearPlan& p, long long M, int N, long lon
     job.idesc = make_idesc_elem(128 * ctas, p.bn, 0, 1);
     const cudaError_t e = by_map || p.splits > 1 ? launch_tiles<kLinearGatedInput, kOps16, true, 1>(p.pair, maps, job, sm_count, stream)
                                                  : launch_tiles<kLinearGatedInput, kOps16, false, 1>(p.pair, maps, job, sm_count, stream);
-    return join<true>(e, p, epi, parts, M, N, stream);
+    return join<true>(e, kOps16, p, epi, parts, M, N, stream);
 }
 
 }  // namespace terra

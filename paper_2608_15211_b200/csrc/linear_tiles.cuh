@@ -200,9 +200,24 @@ __device__ __forceinline__ Pair finish2(Pair d, Pair bias, Pair x_scale, Pair w_
     return padd(act2<ACT>(z), in);
 }
 __device__ __forceinline__ Pair elems2(uint32_t v) { const float2 t = elem2_to_float2(v); return pair_of(t.x, t.y); }
-// A sum as the matrix instructions leave it: fp32, of 8-bit integers 32-bit ones (exact: at most 2^16 products of at most 2^14), rounded to fp32 here
+// A sum as the matrix instructions leave it: fp32, of 8-bit integers 32-bit ones (exact: at most 2^16 products of at most 2^14), rounded to fp32 here.
+// Parts of a split sum keep their form and are added up in it: SumOf.
 template <int OPS>
 __device__ __forceinline__ float sum_value(uint32_t v) { return OPS == kOpsI8 ? __int2float_rn((int)v) : __uint_as_float(v); }
+template <bool WHOLE> struct SumOf { typedef float Type; typedef float4 Four; };
+template <> struct SumOf<true> { typedef int Type; typedef int4 Four; };
+// Adds a part's four columns from `col` of N on.
+template <bool WHOLE>
+__device__ __forceinline__ void part4(const float* p, int col, int N, typename SumOf<WHOLE>::Type (&v)[4]) {
+    if ((N & 3) == 0) {
+        const typename SumOf<WHOLE>::Four t = *reinterpret_cast<const typename SumOf<WHOLE>::Four*>(p);
+        v[0] += t.x; v[1] += t.y; v[2] += t.z; v[3] += t.w;
+    } else {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            if (col + c < N) v[c] += reinterpret_cast<const typename SumOf<WHOLE>::Type*>(p)[c];
+    }
+}
 __device__ __forceinline__ uint32_t pack2(Pair p) { float a, b; split_pair(p, a, b); return pack_elem(a, b); }
 
 __device__ __forceinline__ void prefetch_l1(const float* p) { asm volatile("prefetch.global.L1 [%0];\n" ::"l"(p)); }
@@ -793,7 +808,7 @@ __global__ void __launch_bounds__(kThreads, 1) linear_kernel(const __grid_consta
                             tmem_ld16(lane_tmem + buf * kAccCols + (GATED ? column(64 * chunk, c - 64 * chunk) : c) + 16 * p, t);
                             tmem_ld_wait();
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) f[i] = sum_value<OPS>(t[i]);
+                            for (int i = 0; i < 16; ++i) f[i] = __uint_as_float(t[i]);         // (whole numbers stay what they are)
                             put_sums(tile, lane, p, f);
                         }
                         __syncwarp();
