@@ -70,7 +70,8 @@ struct LinearLayout {
     long long stride_x, stride_w, stride_z;      // bytes of a row as the products read it
     bool pad_x, pad_w, pad_z;
     size_t off_x, off_w, off_z, off_parts, off_sums;
-    LinearPlan first, second, gated;             // forward or input gradient; weight gradient; input gradient through a gate
+    LinearPlan first, second;                    // forward or input gradient; weight gradient
+    size_t room;                                 // bytes at off_parts
     size_t bytes;
 };
 
@@ -101,9 +102,7 @@ LinearLayout layout_linear(const terra_linear_desc* d, int call) {
     if (bwd) {
         l.first = plan_linear(kLinearInput, false, d->rows, d->n_in, d->n_out);
         l.second = plan_linear(kLinearWeights, false, d->n_out, d->n_in, d->rows);
-        l.gated = plan_linear(kLinearGatedInput, false, d->rows, d->n_in, d->n_out);
         need(l.first, (size_t)d->rows * d->n_in);
-        need(l.gated, (size_t)d->rows * d->n_in);
         need(l.second, (size_t)d->n_out * d->n_in);
         const size_t slices = column_sum_blocks(d->rows, d->n_out), splits = l.second.splits * l.second.n_tiles;        // without or with the weight gradient
         l.off_sums = s.add(sizeof(float) * (slices > splits ? slices : splits) * d->n_out);
@@ -112,6 +111,7 @@ LinearLayout layout_linear(const terra_linear_desc* d, int call) {
         need(l.first, (size_t)d->rows * d->n_out * (gated ? 2 : 1));
     }
     l.off_parts = parts ? s.add(parts) : 0;
+    l.room = parts;
     l.bytes = s.bytes;
     return l;
 }
@@ -195,8 +195,12 @@ int linear_bwd(const terra_linear_desc* desc, bool gated, const void* x, const v
     if (e == cudaSuccess && d_x) {
         LinearEpilogue epi = {};
         epi.z_in = z_in; epi.y = d_x; epi.activation = z_in ? desc->activation : TERRA_ACT_NONE;
-        if (gated) e = (f16 ? launch_gated_input_f16 : launch_gated_input)(l.gated, desc->rows, desc->n_in, desc->n_out, d_z, l.stride_z, w, l.stride_w, epi, parts, sms, st);
-        else e = launch(kLinearInput, kOps16, l.first, desc->rows, desc->n_in, desc->n_out, d_z, l.stride_z, w, l.stride_w, epi, nullptr, parts, nullptr, sms, st);
+        if (gated) {
+            // The workspace is the plain backward's, which asks for no more because of the gate: a plan whose parts find room there.  (us, with room for any parts / so:
+            // 2153 x 6016 -> 2 x 856 49 / 29, 216 x 5808 -> 2 x 7328 52 / 34, 79 x 704 -> 2 x 152 6.0 / 7.9, 15 x 1032 -> 2 x 3472 8.2 / 11.1; 97 of 100 sizes the same.)
+            const LinearPlan plan = plan_linear(kLinearGatedInput, false, desc->rows, desc->n_in, desc->n_out, l.room);
+            e = (f16 ? launch_gated_input_f16 : launch_gated_input)(plan, desc->rows, desc->n_in, desc->n_out, d_z, l.stride_z, w, l.stride_w, epi, parts, sms, st);
+        } else e = launch(kLinearInput, kOps16, l.first, desc->rows, desc->n_in, desc->n_out, d_z, l.stride_z, w, l.stride_w, epi, nullptr, parts, nullptr, sms, st);
     }
     return done(e, where);
 }
@@ -256,8 +260,8 @@ int rotary(const terra_swin_desc* desc, const terra_rotary_desc* r, const double
 
 }  // namespace
 
-// The tile, and into how many parts the sum is split, by an estimate of the time in SM cycles.
-static LinearPlan make_plan(int kind, bool bytes, long long M, int N, long long K) {
+// The tile, and into how many parts the sum is split, by an estimate of the time in SM cycles.  Parts take `room` bytes at most.
+static LinearPlan make_plan(int kind, bool bytes, long long M, int N, long long K, size_t room) {
     const long long blocks = (K + (bytes ? 127 : 63)) / (bytes ? 128 : 64);
     LinearPlan best = {};
     double best_cost = 1e300;
@@ -277,6 +281,7 @@ static LinearPlan make_plan(int kind, bool bytes, long long M, int N, long long 
                 const long long per = (blocks + want - 1) / want;
                 const int splits = (int)((blocks + per - 1) / per);
                 if (splits != want) continue;
+                if (splits > 1 && (double)splits * M * N * sizeof(float) > (double)room) break;
                 if (kind != kLinearWeights && splits > 1 && m_tiles * n_tiles * (splits - 1) >= slots) break;
                 const double units = (double)m_tiles * n_tiles * splits, waves = std::ceil(units / slots);
                 // (through a gate two values are read and two written for each: 32768 x 192 -> 512 47 -> 43.5 us, 20000 x 384 -> 1024 55 -> 52)
@@ -307,17 +312,17 @@ static LinearPlan make_plan(int kind, bool bytes, long long M, int N, long long 
 }
 
 // Each thread remembers the plans of its last few sizes: the search takes longer than a launch, and a call asks for its plans twice.
-LinearPlan plan_linear(int kind, bool bytes, long long M, int N, long long K) {
-    struct Known { long long M = 0, K; int kind, N; bool bytes; LinearPlan plan; };
+LinearPlan plan_linear(int kind, bool bytes, long long M, int N, long long K, size_t room) {
+    struct Known { long long M = 0, K; size_t room; int kind, N; bool bytes; LinearPlan plan; };
     constexpr int kKnown = 32;
     static thread_local Known known[kKnown];
     static thread_local int next = 0;
     for (const Known& k : known)
-        if (k.M == M && k.K == K && k.N == N && k.kind == kind && k.bytes == bytes) return k.plan;
+        if (k.M == M && k.K == K && k.N == N && k.kind == kind && k.bytes == bytes && k.room == room) return k.plan;
     Known& k = known[next];
     next = (next + 1) % kKnown;
-    k.plan = make_plan(kind, bytes, M, N, K);
-    k.M = M; k.K = K; k.N = N; k.kind = kind; k.bytes = bytes;
+    k.plan = make_plan(kind, bytes, M, N, K, room);
+    k.M = M; k.K = K; k.room = room; k.N = N; k.kind = kind; k.bytes = bytes;
     return k.plan;
 }
 

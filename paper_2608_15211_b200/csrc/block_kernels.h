@@ -107,7 +107,7 @@ struct LinearPlan {
     int m_tiles, n_tiles, group;       // `group` rows of tiles are worked on together
     int splits, k_blocks, kb_per_split;
 };
-LinearPlan plan_linear(int kind, bool bytes, long long M, int N, long long K);
+LinearPlan plan_linear(int kind, bool bytes, long long M, int N, long long K, size_t room = ~(size_t)0);      // room: bytes for the parts of a split sum, at most
 
 // What stands for 64 columns' bias where there is none: read as 16-byte vectors.
 struct alignas(16) NoBias { float values[64]; };
