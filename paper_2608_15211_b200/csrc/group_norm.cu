@@ -332,20 +332,22 @@ __global__ void __launch_bounds__(kBlock, blocks(E, 1)) group_stats_kernel(const
     }
 }
 
-// stats[sample][group] = (mean, rstd), a block to each: its warps join a part of the entries each, the first one those
+// stats[sample][group] = (mean, rstd), a block to each (groups x samples of them: their product may be more than a grid's first dimension takes): its warps
+// join a part of the entries each, the first one those
 __global__ void __launch_bounds__(kBlock) group_stats_join_kernel(const __grid_constant__ Pass p, int entries) {
     __shared__ Moments warps[kBlock / 32];
     let_dependents_start();
     wait_for_prerequisites();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, share = (entries + kBlock / 32 - 1) / (kBlock / 32), first = min(entries, warp * share);
-    const float* from = p.partial + 3ll * ((long long)blockIdx.x * entries + first);
+    const long long at = (long long)blockIdx.y * p.groups + blockIdx.x;
+    const float* from = p.partial + 3 * (at * entries + first);
     Moments m = joined(min(share, entries - first), [&](int i) { return Moments{from[3 * i], from[3 * i + 1], from[3 * i + 2]}; });
     if (lane == 0) warps[warp] = m;
     __syncthreads();
     if (warp) return;
     m = joined_lanes(lane < kBlock / 32 ? warps[lane] : Moments{0.f, 0.f, 0.f});
     if (lane) return;
-    float* out = p.stats + 2 * ((long long)p.first * p.groups + blockIdx.x);
+    float* out = p.stats + 2 * ((long long)p.first * p.groups + at);
     out[0] = m.mean;
     out[1] = rsqrtf((float)((double)m.m2 * p.per_value) + p.eps);
 }
@@ -902,7 +904,7 @@ cudaError_t forward(const GroupNormArgs& a, const GroupNormPlan& plan, cudaStrea
     return over_samples<E>(pass_of(a, plan), plan, [&](const Pass& p, dim3 grid) {
         constexpr size_t kRing = E == 8 ? kRingFwd : 0, kMoments = sizeof(float) * kBlock * (2 * E + 1);
         cudaError_t e = launch("group_stats_kernel", group_stats_kernel<E>, grid, kBlock, 0, kRing > kMoments ? kRing : kMoments, stream, p);
-        if (e == cudaSuccess) e = launch("group_stats_join_kernel", group_stats_join_kernel, dim3((unsigned)(p.samples * p.groups)), kBlock, 0, 0, stream, p, plan.chunks * plan.pieces);
+        if (e == cudaSuccess) e = launch("group_stats_join_kernel", group_stats_join_kernel, dim3((unsigned)p.groups, (unsigned)p.samples), kBlock, 0, 0, stream, p, plan.chunks * plan.pieces);
         if (e == cudaSuccess) e = launch("group_apply_kernel", group_apply_kernel<E>, grid, kBlock, 0, kRing, stream, p);
         return e;
     });
