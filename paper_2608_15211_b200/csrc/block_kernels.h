@@ -66,6 +66,7 @@ struct GroupNormPlan {
     int slab, slabs, pieces;           // channels of a block; blocks along the channels; of them to a group (1: whole groups)
     int chunks;                        // blocks along a sample's tokens
     int cluster, held;                 // blocks that hold a sample's slab in one launch (0: several launches), and vectors of a thread in shared memory (0: in registers)
+    size_t smem;                       // shared memory of such a block
     bool backward;
     long long chunk;                   // tokens of a block
     size_t off_sums, bytes;            // workspace

@@ -38,6 +38,8 @@ __host__ __device__ constexpr int deep(int elems, int tensors) { return elems ==
 // Blocks of an SM, and stages of a block: kBlock x 4 vectors of 16 bytes each, of x and, backward, of d_y.
 constexpr int kStage = kBlock * deep(8, 1) * 16;
 constexpr int kKeepFwd = 8, kKeepBwd = 4, kMostCluster = 8;        // vectors that a thread of the kernels for small samples holds; their blocks that share a sample's slab
+constexpr int kSmallBlocksSm = 2;      // those kernels' blocks on an SM, by their registers
+constexpr long long kMostHeld = 176 * 1024, kBlockSmem = 227 * 1024, kSmSmem = 228 * 1024;        // bytes of vectors that a block of theirs holds; of a block; of an SM
 constexpr int kMostSamples = 65535;
 constexpr int kFewSamples = 8;         // so many samples' sums are added up one after the other
 // The most blocks that the kernels for small samples are taken for, forward and backward.  us, they / three launches: forward 16 x 1024 x 320 16.6 / 23.1,
@@ -613,7 +615,7 @@ __device__ __forceinline__ float at_rank(const float* mine, int rank) {        /
 }
 
 template <int E, int KEEP>
-__global__ void __launch_bounds__(kBlock, 2) group_small_kernel(const __grid_constant__ Pass p) {
+__global__ void __launch_bounds__(kBlock, kSmallBlocksSm) group_small_kernel(const __grid_constant__ Pass p) {
     extern __shared__ __align__(128) uint8_t shared[];
     float *mean_of = reinterpret_cast<float*>(shared), *m2_of = mean_of + kBlock * E, *count_of = m2_of + kBlock * E, *moments = count_of + kBlock, *stats = moments + 3 * (p.slab / p.per_group);
     constexpr int kPairs = Channels<E>::kPairs;
@@ -711,7 +713,7 @@ __global__ void __launch_bounds__(kBlock, 2) group_small_kernel(const __grid_con
 
 // d_weight and d_bias of one sample come out at once; of more samples their sums, for group_bwd_params_kernel.
 template <int E, int KEEP>
-__global__ void __launch_bounds__(kBlock, 2) group_small_bwd_kernel(const __grid_constant__ Pass p) {
+__global__ void __launch_bounds__(kBlock, kSmallBlocksSm) group_small_bwd_kernel(const __grid_constant__ Pass p) {
     extern __shared__ __align__(128) uint8_t shared[];
     float *rows_sums = reinterpret_cast<float*>(shared), *mine = rows_sums + 2 * kBlock * E, *total = mine + 2 * p.slab, *group_sums = total + 2 * p.slab;
     constexpr int kPairs = Channels<E>::kPairs;
@@ -850,10 +852,8 @@ Pass pass_of(const GroupNormArgs& a, const GroupNormPlan& plan) {
     p.rows = plan.rows;
     p.slab = plan.slab;
     p.pieces = plan.pieces;
-    const int per_slab = plan.slab / p.per_group;
-    const size_t sums = sizeof(float) * (plan.backward ? 2ull * kBlock * plan.elems + 4ull * plan.slab + 2ull * per_slab : kBlock * (2ull * plan.elems + 1) + 5ull * per_slab);
-    p.room = (int)((sums + 127) / 128 * 128);
     p.half = plan.held * kBlock * 16;
+    p.room = (int)plan.smem - (plan.backward ? 2 : 1) * p.half;
     p.eps = a.eps;
     p.per_value = 1. / ((double)a.tokens * p.per_group);
     return p;
@@ -898,8 +898,8 @@ cudaError_t forward(const GroupNormArgs& a, const GroupNormPlan& plan, cudaStrea
     if (plan.cluster)
         return over_samples<E>(pass_of(a, plan), plan, [&](const Pass& p, dim3 grid) {
             if constexpr (E == 8)
-                if (plan.held) return launch("group_small_kernel", group_small_kernel<8, 0>, grid, kBlock, plan.cluster, (size_t)p.room + p.half, stream, p);
-            return launch("group_small_kernel", group_small_kernel<E, kKeepFwd>, grid, kBlock, plan.cluster, (size_t)p.room, stream, p);
+                if (plan.held) return launch("group_small_kernel", group_small_kernel<8, 0>, grid, kBlock, plan.cluster, plan.smem, stream, p);
+            return launch("group_small_kernel", group_small_kernel<E, kKeepFwd>, grid, kBlock, plan.cluster, plan.smem, stream, p);
         });
     return over_samples<E>(pass_of(a, plan), plan, [&](const Pass& p, dim3 grid) {
         constexpr size_t kRing = E == 8 ? kRingFwd : 0, kMoments = sizeof(float) * kBlock * (2 * E + 1);
@@ -915,8 +915,8 @@ cudaError_t backward(const GroupNormArgs& a, const GroupNormPlan& plan, cudaStre
     if (plan.cluster) {
         const cudaError_t e = over_samples<E>(pass_of(a, plan), plan, [&](const Pass& p, dim3 grid) {
             if constexpr (E == 8)
-                if (plan.held) return launch("group_small_bwd_kernel", group_small_bwd_kernel<8, 0>, grid, kBlock, plan.cluster, (size_t)p.room + 2 * p.half, stream, p);
-            return launch("group_small_bwd_kernel", group_small_bwd_kernel<E, kKeepBwd>, grid, kBlock, plan.cluster, (size_t)p.room, stream, p);
+                if (plan.held) return launch("group_small_bwd_kernel", group_small_bwd_kernel<8, 0>, grid, kBlock, plan.cluster, plan.smem, stream, p);
+            return launch("group_small_bwd_kernel", group_small_bwd_kernel<E, kKeepBwd>, grid, kBlock, plan.cluster, plan.smem, stream, p);
         });
         if (e != cudaSuccess || a.samples == 1) return e;
         return launch("group_bwd_params_kernel", group_bwd_params_kernel, dim3((unsigned)(a.channels + 31) / 32), 1024u, 0, 0, stream, pass_of(a, plan));
@@ -956,13 +956,16 @@ GroupNormPlan plan_group_norm(int samples, long long tokens, int channels, int g
         p.pieces = (per_group + most - 1) / most;
         p.slabs = p.pieces * groups;
     }
-    // Samples whose slabs clusters hold: slabs of as few whole groups as make whole vectors, of 64 bytes a token at least.
+    // Samples whose slabs clusters hold: slabs of as few whole groups as make whole vectors, of 64 bytes a token at least.  Shared memory: a block's sums and its
+    // groups' (as the kernels lay them out), then the vectors that it holds there.
     int unit = per_group;
     while (unit % p.elems) unit += per_group;
     while (2 * unit < 64 && channels % (2 * unit) == 0) unit *= 2;
     if (unit <= most) {
         const int rows = kBlock / (unit / p.elems), keep = rows * (backward ? kKeepBwd : kKeepFwd);
         const long long least = (tokens + keep - 1) / keep, slabs = (long long)samples * (channels / unit);       // blocks of a cluster; clusters
+        const long long floats = backward ? 2ll * kBlock * p.elems + 4 * unit + 2 * (unit / per_group) : kBlock * (2ll * p.elems + 1) + 5 * (unit / per_group);
+        const long long sums = (floats * 4 + 127) / 128 * 128;
         if (least <= kMostCluster && least * slabs <= (backward ? kSmallBlocksBwd : kSmallBlocksFwd)) {
             // more blocks of two tokens a thread while they are all on the GPU at a time
             const long long spread = (tokens + 2 * rows - 1) / (2 * rows), fit = 2 * kPlanSms / slabs;
@@ -970,16 +973,20 @@ GroupNormPlan plan_group_norm(int samples, long long tokens, int channels, int g
             if (p.cluster > kMostCluster) p.cluster = kMostCluster;
             if (p.cluster < least) p.cluster = (int)least;
         } else if (p.elems == 8) {
-            // in shared memory, where the blocks of all samples are on the GPU at a time: of the SMs of a cluster of 8 some stay over
-            for (int c = kMostCluster; c >= 1 && !p.cluster; --c) {
-                const long long held = ((tokens + c - 1) / c + rows - 1) / rows, bytes = held * kBlock * 16 * (backward ? 2 : 1) + 24 * 1024;
-                if (bytes > 200 * 1024) break;
-                const long long per_sm = 220 * 1024 / bytes;
-                if (c * slabs <= (per_sm < 4 ? per_sm : 4) * (kPlanSms * 7 / 8)) {
-                    p.cluster = c;
-                    p.held = (int)held;
+            // In shared memory, where the blocks of all samples are on the GPU at a time (of the SMs of a cluster of 8 some stay over) or, two to an SM, in two turns.
+            // us, so / otherwise: 16 x 280 x 960 backward by clusters of 4, 64 blocks that are there at once, 15.2, by clusters of 6 that are not 22.7; in two turns / three
+            // launches 100 x 1720 x 96 30.1 / 34.8, 64 x 371 x 256 backward 23.1 / 36.0, but one block to an SM 16 x 6494 x 80 backward 39.9 / 37.3.
+            for (int turns = 1; turns <= 2 && !p.cluster; ++turns)
+                for (int c = kMostCluster; c >= 1 && !p.cluster; --c) {
+                    const long long held = ((tokens + c - 1) / c + rows - 1) / rows, vectors = held * kBlock * 16 * (backward ? 2 : 1);
+                    if (vectors > kMostHeld || vectors + sums > kBlockSmem) break;
+                    const long long fit = kSmSmem / (vectors + sums + 1024), per_sm = fit < kSmallBlocksSm ? fit : kSmallBlocksSm;     // (1 KB of a block is the system's)
+                    if (turns == 2 && per_sm < kSmallBlocksSm) break;
+                    if (c * slabs <= turns * per_sm * (kPlanSms * 7 / 8)) {
+                        p.cluster = c;
+                        p.held = (int)held;
+                    }
                 }
-            }
         }
         if (p.cluster) {
             p.slab = unit;
@@ -987,6 +994,7 @@ GroupNormPlan plan_group_norm(int samples, long long tokens, int channels, int g
             p.pieces = 1;
             p.across = unit / p.elems;
             p.rows = rows;
+            p.smem = (size_t)(sums + (long long)p.held * kBlock * 16 * (backward ? 2 : 1));
             p.chunks = p.cluster;
             p.chunk = (tokens + p.cluster - 1) / p.cluster;
             p.bytes = backward && samples > 1 ? (sizeof(float) * 2 * samples * (size_t)channels + 255) / 256 * 256 : 0;

@@ -3,6 +3,7 @@ import pytest
 import torch
 
 import paper_2608_15211_b200 as terra
+import tests.test_gpu_group_norm as cases
 from tests.test_gpu_group_norm import check_forward
 
 pytestmark = pytest.mark.gpu
@@ -22,3 +23,10 @@ def test_more_than_2_31_groups():
     assert stats[..., 1].min() > 0
     del x, y, stats, parts
     torch.cuda.empty_cache()           # 50 GB
+
+
+# samples in shared memory: at a time by smaller clusters, in two turns, nearly all of an SM's, a group to a channel
+@pytest.mark.parametrize("samples,tokens,channels,groups", [(16, 280, 960, 4), (64, 371, 256, 1), (100, 1720, 96, 2), (32, 88, 1784, 2), (2, 2804, 1904, 1904), (100, 64, 1264, 4), (3, 4189, 640, 32)])
+def test_samples_in_shared_memory(samples, tokens, channels, groups):
+    cases.test_forward(samples, tokens, channels, groups, torch.bfloat16)
+    cases.test_backward(samples, tokens, channels, groups, torch.float16)
