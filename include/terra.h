@@ -436,8 +436,9 @@ int terra_group_norm_workspace_bytes(const terra_group_norm_desc* desc, int back
  *   y              elem [samples, tokens, channels]   may be x
  *   stats          fp32 [samples, groups, 2]          mean and rstd, for the backward
  * (The order of the sums, and with it their last bits, goes by the sizes of the whole call, the number of samples among them.)
- * The variance is that of the group's values about their mean, however far that lies from 0.  A group with a value that is not finite, or whose deviations have squares
- * beyond fp32, gives what the formula gives: NaN, or act(bias).
+ * The variance is that of the group's values about their mean, however far that lies from 0.  A group with a value that is not finite gives NaN.  Squared deviations
+ * are added up in fp32: where their sum leaves its range (deviations of 1e16 of 4e6 values, of 1e19 of four) rstd is 0 and y act(bias), and those below 1e-38 lose
+ * digits (rstd above 1e19).
  */
 int terra_group_norm_fwd(const terra_group_norm_desc* desc, const void* x, const float* weight, const float* bias, void* y, float* stats, void* workspace,
                          size_t workspace_bytes, void* stream);

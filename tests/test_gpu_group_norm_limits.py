@@ -30,3 +30,17 @@ def test_more_than_2_31_groups():
 def test_samples_in_shared_memory(samples, tokens, channels, groups):
     cases.test_forward(samples, tokens, channels, groups, torch.bfloat16)
     cases.test_backward(samples, tokens, channels, groups, torch.float16)
+
+
+@pytest.mark.parametrize("tokens", [40, 3000, 50000])
+def test_sums_of_squares_beyond_the_range(tokens):
+    # deviations of 2^63: four of their squares are more than fp32 holds; of 2^53 in the next group 2^22 of them would be
+    x = torch.zeros(1, tokens, 16, device="cuda", dtype=torch.bfloat16)
+    x[:, 0::2, :8], x[:, 1::2, :8] = 2.0 ** 63, -2.0 ** 63
+    x[:, 0::2, 8:], x[:, 1::2, 8:] = 2.0 ** 53, -2.0 ** 53
+    w, b = torch.ones(16, device="cuda"), torch.linspace(-1, 1, 16, device="cuda")
+    y, stats = terra.terra_group_norm_fwd(x, w, b, 2)
+    assert stats[0, 0, 1] == 0 and torch.equal(y[0, :, :8], b[:8].to(torch.bfloat16).expand(tokens, 8))
+    # means of 0 within the joinings' roundings of values of that size
+    assert stats[0, 0, 0].abs() <= 2.0 ** 63 * 64 * 2.0 ** -24 and stats[0, 1, 0].abs() <= 2.0 ** 53 * 64 * 2.0 ** -24
+    assert abs(stats[0, 1, 1].item() * 2.0 ** 53 - 1) <= 2.0 ** -17
