@@ -10,8 +10,8 @@
 // A thread's mean and squared deviations from it are updated value by value (Welford 1962), those of several threads or blocks joined by the mean of all and the
 // deviations about it, so that nothing cancels however far the mean lies from 0; all in fp32.
 //
-// What bounds it: HBM in large samples (2 x 2203200 x 128, 32 groups, silu: 575 us, 1.7 GB read twice and written; backward 930), the first pass at 5.2 TB/s, the second at 6.1; in small ones
-// launches and latency (2048 x 96: one launch, 7.5 us).  By loads into registers instead of the copy engine's stages the first pass took 200 us of 2203200 x 128 instead of 117.
+// What bounds it: HBM in large samples (2 x 2203200 x 128, 32 groups, silu, a call on its own: 575 us, 1.1 GB read twice and written; backward 950), the first pass at 5.2 TB/s, the second at
+// 6.1; in small ones launches and latency (2048 x 96: one launch, 7.5 us).  By loads into registers instead of the copy engine's stages the first pass took 200 us of 2203200 x 128 instead of 117.
 #include "block_act.cuh"
 #include "block_kernels.h"
 #include "elem_vec.cuh"
@@ -33,7 +33,7 @@ namespace {
 constexpr int kBlock = 256;
 // Tokens that a thread has of a stage or, where its vectors are smaller than 16 bytes, reads at a time of each of `tensors`.  us of 100000 x 1001 of
 // 7 groups and of 300000 x 131 of one: forward 563 and 234 with 4 of them and 3 blocks of an SM, 440 and 125 with 16 and 4; backward 1371 and 403 with
-// 4 and 2, 818 and 221 with 16 and 3, 759 and 206 with 8 and 4.
+// 4 and 2, 818 and 221 with 16 and 3, 759 and 206 with 8 and 4 (800 and 221 since rstd is a factor of its own in the second pass).
 __host__ __device__ constexpr int deep(int elems, int tensors) { return elems == 8 ? 4 : 16 / tensors; }
 // Blocks of an SM, and stages of a block: kBlock x 4 vectors of 16 bytes each, of x and, backward, of d_y.
 constexpr int kStage = kBlock * deep(8, 1) * 16;

@@ -5,9 +5,10 @@
 // output; of two CTAs on a tile one brings the gate's weights, the other the up rows.  Nothing but y (and z where it is kept) is written.  Backward: the tile
 // is the gradient d of y; the epilogue reads g and u and writes d u act'(g) and d act(g) where z lies, so d itself never reaches memory.
 //
-// What bounds it: forward, the tensor pipe where the sum is long (32768 x 1024 -> 4096 337 us, busy in 92 % of the cycles, in 8-bit integers 184 us, 79 %; 156672 x 4096 -> 8192 6.6 ms
-// in 8 bits, 3190 TFLOP/s), writes where z is kept (550800 x 384 -> 1024 955 us for 3.4 GB); backward, operands and z that share the way into the SMs (156672 x 1024 -> 2752
-// 925 us, the pipe busy in 57 % of the cycles, HBM at 4.6 TB/s; 550800 x 384 -> 1024 905 us, 5.4 TB/s).
+// What bounds it, a call on a cool GPU (one after the other over seconds, under the power cap, in brackets): forward, the tensor pipe where the sum is long (32768 x 1024 -> 4096 337 us,
+// busy in 92 % of the cycles, in 8-bit integers 184 us, 79 %; 156672 x 4096 -> 8192 in 8 bits 6.5 ms, 3240 TFLOP/s (7.5 ms)), the epilogue in 8 bits where it is short (550800 x 384 ->
+// 1024 800 us, in 16 bits 715), writes where z is kept (550800 x 384 -> 1024 955 us (1.1 ms) for 3.4 GB); backward, operands and z that share the way into the SMs (156672 x 1024 -> 2752
+// 925 us, with the weight gradient 1.6 ms (2.0), the pipe busy in 57 % of the cycles, HBM at 4.6 TB/s; 550800 x 384 -> 1024 905 us, 5.4 TB/s).
 #include "linear_tiles.cuh"
 
 #ifdef TERRA_ELEM_F16

@@ -1,23 +1,24 @@
 // Products of a Transformer block on the tcgen05 tensor cores, D[M, N] = sum over k of A(m, k) B(n, k), with what follows them in the epilogue:
-//   forward          A = x [rows, n_in], B = w [n_out, n_in]: z = D (scales) + bias, y = act(z) + residual; 16-bit or e4m3 operands
-//   input gradient   A = d_z [rows, n_out], B = w read along n_in: d_x = D act'(z_in)
+//   forward          A = x [rows, n_in], B = w [n_out, n_in]: z = D (scales) + bias, y = act(z) + residual; operands of 16 bits, e4m3 or 8-bit integers
+//   gated forward    B = the gate's rows of w and as many up rows: [g, u] = D (scales) + bias, y = act(g) u; operands of 16 bits or 8-bit integers
+//   input gradient   A = d_z [rows, n_out], B = w read along n_in: d_x = D act'(z_in), or through a gate z_in = [g, u]: [D u act'(g), D act(g)]
 //   weight gradient  A = d_z and B = x, both read along their features, summed over the rows: d_w = D in fp32
 // An operand whose memory runs along k is "K-major", one that runs along m or n "MN-major"; TMA brings either in 128-byte-swizzled rows,
 // and the shared-memory descriptors say which it is, so nothing is transposed.
 //
 // Persistent: a unit is one output tile (of one part of the sum, where it is split).  PAIR: two CTAs on neighbouring SMs work on a
 // tile of 256 rows with tcgen05.mma.cta_group::2, each with its 128 rows of A and half of the columns of B; alone, a CTA has 128 rows.  Five
-// (or three) stages of 64 k (128 in e4m3) each, two accumulators in TMEM, so that the epilogue of a tile runs under the products of the next.
+// (or four, or three) stages of 64 k (128 of 8 bits) each, two accumulators in TMEM, so that the epilogue of a tile runs under the products of the next.
 // The epilogue works on a warp's 32 rows x 64 columns at a time, a row to a thread, two columns to an instruction; the residual comes and the
 // results go as tiles in shared memory that the copy engine moves (rows that are no multiples of 16 bytes: the warp itself, in whole rows).
 //
-// The tensor cores' sum over k is cut off, not rounded to nearest, and its error grows with the number of steps, four a stage: 1.9e-8 of the 2-norm a step
+// Sums of 8-bit integers are exact.  The tensor cores' sum in fp32 over k is cut off, not rounded to nearest, and its error grows with the number of steps, four a stage: 1.9e-8 of the 2-norm a step
 // on N(0, 1), 1.05e-7 where all terms have one sign.  The weight gradient, a sum over all rows that comes out in fp32, therefore leaves TMEM every kLinearChunk
 // stages and is added up in registers (156672 rows of N(0, 1) in fp16: 3.6e-7 off in the 2-norm, with 16 stages 1.2e-6, at the same time).  The other products,
 // whose results are rounded to 16 bits, leave it every kLinearLongChunk stages: terms of one sign are then 1.3e-5 off at most, a fortieth of fp16's half
 // step.  (4096 features in one go 2.6e-5, 65536 4.3e-4.  156672 x 4096 -> 4096 takes 3399 us instead of 3367 so, with a residual 3538 instead of 3505.)
 //
-// What bounds it: the tensor pipe where the sum is long (156672 x 4096 -> 4096 3.40 ms, 1546 TFLOP/s, the pipe busy in 89 % of the cycles; e4m3 to 16384 with
+// What bounds it, a call on a cool GPU: the tensor pipe where the sum is long (156672 x 4096 -> 4096 3.40 ms, 1546 TFLOP/s, the pipe busy in 89 % of the cycles; e4m3 to 16384 with
 // GELU 7.2 ms, 2920 TFLOP/s), over seconds the power cap (4.1 and 9.0 ms); the epilogue where it is short (550800 x 384 -> 1536 with GELU 0.85 ms, two
 // reciprocals or exponentials an output in a unit that takes 16 a clock and SM, busy in half the cycles), with z besides the writes: 3.4 GB, of which HBM
 // takes 3.9 GB a ms (0.98 ms).  Rows that are no multiples of 16 bytes: the warps' copies (2203200 x 256 -> 372 0.64 ms, -> 384 0.56).
