@@ -175,29 +175,15 @@ cudaError_t launch_linear(int kind, int ops, const LinearPlan& p, long long M, i
                    (epi.z && !encode_map(&maps.z, epi.z, N, M, 2ll * N, 2, 32, wide))))
         return cudaErrorInvalidValue;
     Job job{};
-    job.M = M;
-    job.N = N;
-    job.bn = job.wide = p.bn;
-    job.m_tiles = p.m_tiles;
-    job.n_tiles = p.n_tiles;
-    job.group = p.group < p.m_tiles ? p.group : p.m_tiles;
-    job.groups = (p.m_tiles + job.group - 1) / job.group;
-    job.by_group = Divider((uint32_t)job.group);
-    job.by_n_tiles = Divider((uint32_t)p.n_tiles);
-    job.by_groups = Divider((uint32_t)job.groups);
-    job.splits = p.splits;
-    job.k_blocks = p.k_blocks;
-    job.kb_per_split = p.kb_per_split;
-    if ((long long)job.groups * job.group * p.n_tiles * p.splits > 0x3fffffffLL) return cudaErrorInvalidConfiguration;
+    if (!set_job(job, p, p.bn, M, N, epi, parts)) return cudaErrorInvalidConfiguration;
     job.boxes_b = (cols + 63) / 64;
     job.bytes_b = b_mn ? job.boxes_b * (kOperand / 2) : cols * 128;
     job.idesc = ops == kOpsI8   ? make_idesc_i8(128 * ctas, p.bn)
               : ops == kOpsE4m3 ? make_idesc_f16(128 * ctas, p.bn, 0, 0)      // e4m3 has format number 0, as fp16 has in its kind
                                 : make_idesc_elem(128 * ctas, p.bn, a_mn ? 1 : 0, b_mn ? 1 : 0);
-    job.e = epi;
     const int a_splits = epi.a_sums ? p.splits * p.n_tiles : 0;
     if (a_splits > 1) job.e.a_sums = a_parts;
-    job.e.sums = p.splits > 1 ? parts : kind == kLinearWeights ? out : nullptr;
+    if (kind == kLinearWeights && p.splits == 1) job.e.sums = out;
     // (a part of a split sum goes neither way)
     const bool map = by_map || p.splits > 1;
     cudaError_t e;

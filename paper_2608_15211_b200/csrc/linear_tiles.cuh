@@ -1223,5 +1223,26 @@ cudaError_t launch_one(const Maps& maps, Job& job, int sm_count, cudaStream_t st
     return e;
 }
 
+// What a kernel's job takes from its plan; `wide`: columns of the output of a tile.  Whether its units can be numbered.
+inline bool set_job(Job& job, const LinearPlan& p, int wide, long long M, int N, const LinearEpilogue& epi, float* parts) {
+    job.M = M;
+    job.N = N;
+    job.bn = p.bn;
+    job.wide = wide;
+    job.m_tiles = p.m_tiles;
+    job.n_tiles = p.n_tiles;
+    job.group = p.group < p.m_tiles ? p.group : p.m_tiles;
+    job.groups = (p.m_tiles + job.group - 1) / job.group;
+    job.by_group = Divider((uint32_t)job.group);
+    job.by_n_tiles = Divider((uint32_t)p.n_tiles);
+    job.by_groups = Divider((uint32_t)job.groups);
+    job.splits = p.splits;
+    job.k_blocks = p.k_blocks;
+    job.kb_per_split = p.kb_per_split;
+    job.e = epi;
+    job.e.sums = p.splits > 1 ? parts : nullptr;
+    return (long long)job.groups * job.group * p.n_tiles * p.splits <= 0x3fffffffLL;
+}
+
 }  // namespace
 }  // namespace terra
