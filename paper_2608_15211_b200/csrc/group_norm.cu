@@ -33,7 +33,7 @@ namespace {
 constexpr int kBlock = 256;
 // Tokens that a thread has of a stage or, where its vectors are smaller than 16 bytes, reads at a time of each of `tensors`.  us of 100000 x 1001 of
 // 7 groups and of 300000 x 131 of one: forward 563 and 234 with 4 of them and 3 blocks of an SM, 440 and 125 with 16 and 4; backward 1371 and 403 with
-// 4 and 2, 818 and 221 with 16 and 3, 759 and 206 with 8 and 4 (800 and 221 since rstd is a factor of its own in the second pass).
+// 4 and 2, 818 and 221 with 16 and 3, 759 and 206 with 8 and 4 (790 and 214 since rstd is a factor of its own in the second pass).
 __host__ __device__ constexpr int deep(int elems, int tensors) { return elems == 8 ? 4 : 16 / tensors; }
 // Blocks of an SM, and stages of a block: kBlock x 4 vectors of 16 bytes each, of x and, backward, of d_y.
 constexpr int kStage = kBlock * deep(8, 1) * 16;
